@@ -118,7 +118,7 @@ def _quantise_rows(x):
     x = x.float()
     amax = x.abs().amax(-1, keepdim=True)
     codes = torch.where(amax > 0, torch.round(x * 127.0 / amax), torch.zeros_like(x))
-    return codes.to(torch.int8), (amax / 127.0).squeeze(-1)
+    return codes.to(torch.int8), torch.div(amax, torch.full_like(amax, 127.0)).squeeze(-1)     # (a plain number's reciprocal would be multiplied by)
 
 
 def _random_cache(gen, batch, seq, heads, dim):
@@ -137,7 +137,8 @@ def _random_cache(gen, batch, seq, heads, dim):
 def _quantise_matrix(w, group):
     """fp32 [out][in] -> codes int8 in -7 .. 7, scales bf16 [out][in / group]."""
     g = w.view(w.shape[0], -1, group)
-    scales = (g.abs().amax(-1) / 7.0).to(torch.bfloat16)
+    top = g.abs().amax(-1)
+    scales = torch.div(top, torch.full_like(top, 7.0)).to(torch.bfloat16)
     s = scales.float().unsqueeze(-1)
     codes = torch.where(s > 0, torch.round(g / s).clamp(-7, 7), torch.zeros_like(g))
     return codes.to(torch.int8).view_as(w), scales
