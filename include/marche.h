@@ -435,6 +435,85 @@ int marche_attention_two_segment(marche_ctx* ctx, const void* qkv, int ld, int n
                                  void* cache_layer, const uint8_t* is_new, float* score_partial, void* o,
                                  marche_stream stream);
 
+/* ---------------------------------------------------------------- a cache of 8 bits, weights of 4
+ * For decoding of few rows, which is bound by the bytes of the cache and of the weight matrices.  The calls
+ * stand beside marche_scatter_kv, marche_attention and marche_linear and take their sizes from their own
+ * arguments, not from the context's shape; the context gives the element types (16-bit contexts only:
+ * MARCHE_ESHAPE in a fp32 one), the device and the status word.  They need no workspace. */
+
+/* One block's K and V, a value being code * scale with one scale per token and cached head:
+ *   codes   int8  [2][batch][seq_len][n_kv_heads * head_dim]   ([0] holds K, [1] V; -127 .. 127)
+ *   scales  float [2][batch][n_kv_heads][pad], pad = seq_len rounded up to a multiple of 64; the entries
+ *           behind seq_len are neither read for their values nor written
+ * head_dim 64, 80 or 128 and seq_len up to MARCHE_QUANTIZED_MAX_SEQ (MARCHE_ESHAPE otherwise); both arrays
+ * 16-byte aligned device memory of the caller, of the sizes that the two functions return (0 for
+ * dimensions that are not supported). */
+#define MARCHE_QUANTIZED_MAX_SEQ (1 << 24)
+typedef struct {
+  int8_t* codes;
+  float* scales;
+  int32_t batch, seq_len, n_kv_heads, head_dim;
+} marche_quantized_cache;
+size_t marche_quantized_codes_bytes(int batch, int seq_len, int n_kv_heads, int head_dim);
+size_t marche_quantized_scales_bytes(int batch, int seq_len, int n_kv_heads, int head_dim);
+
+/* Cache write-back with quantisation: k, v bf16 [batch*n] rows with row stride ld_kv, heads side by side.  Per row
+ * and head, amax = max |x|: code = 127 x / amax rounded to nearest, ties to even (of exact arithmetic), scale =
+ * amax / 127 rounded to fp32; a head of zeros gets codes and scale 0, one that holds an infinity or a
+ * NaN gets codes 0 and a NaN scale (it reads back as NaN throughout).  idx device int32 [batch][n]: the
+ * token of each row, NULL: tokens 0 .. n-1 (n <= seq_len).  Rows whose idx is outside 0 .. seq_len-1 (-1, say, where samples have
+ * different numbers of rows) are left out.  The same token twice in one call is undefined.  Rows that are not
+ * named keep their bytes.  ld_kv % 8 == 0, k and v 16-byte aligned (MARCHE_EINVAL). */
+int marche_scatter_kv_quantized(marche_ctx* ctx, const void* k, const void* v, int ld_kv, const int32_t* idx, int n,
+                                const marche_quantized_cache* cache, marche_stream stream);
+
+/* Its inverse: row j of sample b of k_out and v_out (bf16 [batch*n], row stride ld_out) receives code * scale of token
+ * idx[b][j] (NULL: token j), computed in fp32 and rounded once.  Rows whose idx is outside the cache keep
+ * their bytes.  ld_out % 8 == 0, 16-byte aligned outputs (MARCHE_EINVAL). */
+int marche_gather_kv_quantized(marche_ctx* ctx, const marche_quantized_cache* cache, const int32_t* idx, int n,
+                               void* k_out, void* v_out, int ld_out, marche_stream stream);
+
+/* Attention of n query rows per sample over such a cache, unmasked but for a number of keys per sample:
+ *   o[b*n+j][h] = softmax_s(q[b*n+j][h] . K[s][g] / sqrt(head_dim)) V[.][g], s < kv_len[b], g = h / (n_heads / n_kv_heads)
+ *   q       bf16 [batch*n], row stride ld_q, head h at columns h*head_dim; ld_q % 8 == 0, 16-byte aligned
+ *   n       any number of rows from 1 (a single new token) up; 0 enqueues nothing
+ *   kv_len  device int32 [batch] or NULL (all seq_len); clamped to 0 .. seq_len; nothing behind it is looked at.  A
+ *           sample without keys gives zeros.
+ *   o       A [batch*n][n_heads*head_dim] dense, 16-byte aligned
+ * n_heads % n_kv_heads == 0 (MARCHE_EINVAL).  Relevance scores are not taken here: a block that yields them keeps a
+ * 16-bit cache.  Every shape is bit-reproducible. */
+int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, int n_heads,
+                               const marche_quantized_cache* cache, const int32_t* kv_len, void* o, marche_stream stream);
+
+/* A weight matrix [n][k] (outputs, inputs) of 4 bits: w = code * scale, code -8 .. 7, one bf16 scale per output and
+ * `group` neighbouring inputs.  n % 16 == 0, k % 64 == 0, group 32, 64 or 128, k % group == 0 (MARCHE_ESHAPE).
+ *   codes   the size that marche_quantized_weights_bytes returns (0: not supported), in the order in which the kernel
+ *           multiplies: [n/16][k/64][lane 0..31][word 0..3], little-endian words of eight nibbles code + 8.
+ *           With g = lane / 4, t = lane % 4, nibble i of word s (i = r + 4 e, r = 0..3, e = 0, 1; bits 4 r + 16 e up)
+ *           holds output 16 tile + g + 8 (r % 2), input 64 chunk + 32 (s / 2) + 8 t + 4 (s % 2) + 2 (r / 2) + e.
+ *   scales  bf16 [n/16][k/group][16]; *scales_bytes receives their size
+ * Both 16-byte aligned. */
+typedef struct {
+  void* codes;
+  void* scales;
+  int32_t n, k, group;
+} marche_quantized_weights;
+size_t marche_quantized_weights_bytes(int n, int k, int group, size_t* scales_bytes);
+
+/* Lays out w, device float [n][k] dense, in out->codes and out->scales: scale = max |w| / 7 of the group rounded
+ * to bf16, code = w / scale rounded to nearest, ties to even, and clamped to -7 .. 7; a group that holds an infinity
+ * or a NaN gets a NaN scale.  Asynchronous. */
+int marche_quantize_weights(marche_ctx* ctx, const float* w, const marche_quantized_weights* out, marche_stream stream);
+
+/* out = epilogue(a * w^T + bias) with the epilogues and element types of marche_linear; a is A [M][k] with row
+ * stride lda (lda % 8 == 0).  Meant for few rows: 32 share a pass over the matrix, more repeat it; M up to
+ * MARCHE_QUANTIZED_MAX_ROWS (MARCHE_ESHAPE).  fp32 accumulation of exact products; GELU with the exact erf.  The weights
+ * are fetched before the preceding kernel of the stream has finished: they must be complete in memory, as for
+ * marche_linear (synchronise after laying them out, or keep another kernel of the stream in between). */
+#define MARCHE_QUANTIZED_MAX_ROWS 65536
+int marche_linear_quantized(marche_ctx* ctx, const void* a, int lda, int M, const marche_quantized_weights* w,
+                            const float* bias, int epilogue, void* out, marche_stream stream);
+
 /* ---------------------------------------------------------------- tuning
  * Kernel-selection switches of one context.  The defaults (marche_get_tuning after marche_create)
  * are the measured winners on B200; the alternatives exist for measurements and for the tests that

@@ -49,6 +49,15 @@ class MarcheTuning(C.Structure):
                                          "two_segment_attention", "gemm_kernel", "tail_split", "tile_n", "pdl")]
 
 
+class MarcheQuantizedCache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)] + \
+        [(n, C.c_int32) for n in ("batch", "seq_len", "n_kv_heads", "head_dim")]
+
+
+class MarcheQuantizedWeights(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)] + [(n, C.c_int32) for n in ("n", "k", "group")]
+
+
 class MarcheError(RuntimeError):
     def __init__(self, code: int, detail: str = ""):
         self.code = code
@@ -82,6 +91,14 @@ _SIGNATURES = {
     "marche_attention": (C.c_int, [_vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp]),
     "marche_attention_two_segment": (C.c_int, [_vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
     "marche_gather_rows": (C.c_int, [_vp, _vp, _vp, _i, _vp, _vp]),
+    "marche_quantized_codes_bytes": (_sz, [_i, _i, _i, _i]),
+    "marche_quantized_scales_bytes": (_sz, [_i, _i, _i, _i]),
+    "marche_scatter_kv_quantized": (C.c_int, [_vp, _vp, _vp, _i, _vp, _i, _vp, _vp]),
+    "marche_gather_kv_quantized": (C.c_int, [_vp, _vp, _vp, _i, _vp, _vp, _i, _vp]),
+    "marche_attention_quantized": (C.c_int, [_vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp]),
+    "marche_quantized_weights_bytes": (_sz, [_i, _i, _i, C.POINTER(_sz)]),
+    "marche_quantize_weights": (C.c_int, [_vp, _vp, _vp, _vp]),
+    "marche_linear_quantized": (C.c_int, [_vp, _vp, _i, _i, _vp, _vp, _i, _vp, _vp]),
     "marche_staging_bytes": (_sz, [_vp, _i]),
     "marche_step_host": (C.c_int, [_vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _vp, _i, _vp, _i, _f, _vp, _vp, _vp, _vp,
                                    C.POINTER(C.c_int), _i, _vp, _sz, _vp, _sz, _vp]),
@@ -177,6 +194,46 @@ def upload_mar_weights(mar: Dict, dtype: str, device="cuda", operand: str = "f16
     return {name: (_as_operand(torch.as_tensor(mar[name]), mt, name, device) if name == "w_dec_embed" else
                    torch.as_tensor(mar[name]).to(device=device, dtype=torch.float32).contiguous())
             for name in MAR_FIELDS}
+
+
+class QuantizedCache:
+    """One block's K and V in 8 bits: codes int8 [2][B][S][kv_heads * head_dim] and scales fp32
+    [2][B][kv_heads][S rounded up to 64], as marche_quantized_cache lays them out."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, n_kv_heads: int):
+        two, B, S, D = codes.shape
+        assert codes.is_cuda and codes.is_contiguous() and codes.dtype == torch.int8 and two == 2
+        assert n_kv_heads > 0 and D % n_kv_heads == 0
+        assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.float32
+        assert tuple(scales.shape) == (2, B, n_kv_heads, (S + 63) // 64 * 64), "scales [2][B][kv_heads][S rounded up to 64]"
+        self.codes, self.scales = codes, scales
+        self.B, self.S, self.n_kv_heads, self.head_dim = B, S, n_kv_heads, D // n_kv_heads
+        self.c = MarcheQuantizedCache(codes.data_ptr(), scales.data_ptr(), B, S, n_kv_heads, self.head_dim)
+        self.ref = C.addressof(self.c)
+
+    def check_rows(self, t: torch.Tensor, ld: int, n: int, width: int = 0):
+        """B * n rows of `width` (the cache's by default) bf16 values, `ld` values apart, lie in t's storage."""
+        rows = self.B * n
+        assert t.dtype == torch.bfloat16 and t.device == self.codes.device, "bf16 rows on the cache's device"
+        if rows > 0:
+            need = t.storage_offset() + (rows - 1) * ld + (width or self.codes.shape[3])
+            assert 2 * need <= t.untyped_storage().nbytes(), "fewer rows than the call names"
+
+    def index(self, t: Optional[torch.Tensor], n: int) -> Optional[int]:
+        if t is not None:
+            assert t.dtype == torch.int32 and t.numel() >= self.B * n, "int32, one entry for every row"
+        return _ptr(t)
+
+
+class QuantizedWeights:
+    """A weight matrix [N][K] of 4 bits with bf16 scales per group, in marche_quantized_weights' layout."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, N: int, K: int, group: int):
+        assert codes.is_cuda and codes.is_contiguous() and codes.dtype == torch.uint8 and codes.numel() == N * K // 2
+        assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.bfloat16 and scales.numel() == N * (K // group)
+        self.codes, self.scales, self.N, self.K, self.group = codes, scales, N, K, group
+        self.c = MarcheQuantizedWeights(codes.data_ptr(), scales.data_ptr(), N, K, group)
+        self.ref = C.addressof(self.c)
 
 
 class Marche:
@@ -372,6 +429,59 @@ class Marche:
     def gather_rows(self, src, idx, rows_out, stream=None):
         self._check(self.lib.marche_gather_rows(self.h, _ptr(src), _ptr(idx), idx.shape[1], _ptr(rows_out),
                                                 _stream(stream)))
+
+    # ------------------------------------------------------------- a cache of 8 bits, weights of 4
+    def alloc_quantized_cache(self, batch: int, seq_len: int, n_kv_heads: int, head_dim: int) -> QuantizedCache:
+        """An empty cache (codes and scales 0: every row reads back as zeros)."""
+        n_codes = self.lib.marche_quantized_codes_bytes(batch, seq_len, n_kv_heads, head_dim)
+        n_scales = self.lib.marche_quantized_scales_bytes(batch, seq_len, n_kv_heads, head_dim)
+        if n_codes == 0:
+            raise MarcheError(-2)
+        codes = torch.zeros(n_codes, dtype=torch.int8, device="cuda").view(2, batch, seq_len, n_kv_heads * head_dim)
+        scales = torch.zeros(n_scales // 4, dtype=torch.float32, device="cuda").view(2, batch, n_kv_heads, -1)
+        return QuantizedCache(codes, scales, n_kv_heads)
+
+    def scatter_kv_quantized(self, k, v, ld_kv, idx, n, cache: QuantizedCache, stream=None):
+        """k, v: bf16 rows (or columns of wider rows) with row stride ld_kv; idx int32 [B][n] or None (tokens 0 .. n-1)."""
+        cache.check_rows(k, ld_kv, n)
+        cache.check_rows(v, ld_kv, n)
+        self._check(self.lib.marche_scatter_kv_quantized(self.h, k.data_ptr(), v.data_ptr(), ld_kv, cache.index(idx, n), n, cache.ref,
+                                                         _stream(stream)))
+
+    def gather_kv_quantized(self, cache: QuantizedCache, idx, n, k_out, v_out, ld_out, stream=None):
+        cache.check_rows(k_out, ld_out, n)
+        cache.check_rows(v_out, ld_out, n)
+        self._check(self.lib.marche_gather_kv_quantized(self.h, cache.ref, cache.index(idx, n), n, k_out.data_ptr(), v_out.data_ptr(),
+                                                        ld_out, _stream(stream)))
+
+    def attention_quantized(self, q, ld_q, n, n_heads, cache: QuantizedCache, kv_len, o, stream=None):
+        """q: bf16 rows [B*n] (or columns of wider rows) with row stride ld_q; kv_len int32 [B] or None; o dense."""
+        cache.check_rows(q, ld_q, n, n_heads * cache.head_dim)
+        assert o.dtype == self.operand_dtype and o.numel() >= cache.B * n * n_heads * cache.head_dim
+        self._check(self.lib.marche_attention_quantized(self.h, q.data_ptr(), ld_q, n, n_heads, cache.ref, cache.index(kv_len, 1),
+                                                        _ptr(o), _stream(stream)))
+
+    def quantize_weights(self, w: torch.Tensor, group: int, stream=None) -> QuantizedWeights:
+        """w float32 [N][K] -> its layout in 4 bits.  Synchronises, so that it may be used at once."""
+        assert w.dtype == torch.float32
+        N, K = w.shape
+        n_scales = C.c_size_t(0)
+        n_codes = self.lib.marche_quantized_weights_bytes(N, K, group, C.byref(n_scales))
+        if n_codes == 0:
+            raise MarcheError(-2)
+        q = QuantizedWeights(torch.empty(n_codes, dtype=torch.uint8, device="cuda"),
+                             torch.empty(n_scales.value // 2, dtype=torch.bfloat16, device="cuda"), N, K, group)
+        self._check(self.lib.marche_quantize_weights(self.h, _ptr(w), q.ref, _stream(stream)))
+        (stream or torch.cuda.current_stream()).synchronize()
+        return q
+
+    def linear_quantized(self, a, w: QuantizedWeights, bias, epilogue, out, M=None, lda=None, stream=None):
+        M = a.shape[0] if M is None else M
+        lda = a.stride(0) if lda is None else lda
+        assert a.dtype == self.operand_dtype and bias.dtype == torch.float32 and bias.numel() >= w.N
+        assert out.dtype == (self.torch_dtype, torch.float32, self.operand_dtype)[epilogue] and out.numel() >= M * w.N
+        self._check(self.lib.marche_linear_quantized(self.h, a.data_ptr(), lda, M, w.ref, _ptr(bias), epilogue, _ptr(out),
+                                                     _stream(stream)))
 
     def staging_bytes(self, max_new: int) -> int:
         return self.lib.marche_staging_bytes(self.h, max_new)

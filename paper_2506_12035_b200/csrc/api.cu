@@ -845,6 +845,128 @@ int marche_attention(marche_ctx* ctx, const void* q, int ld_q, int n, const void
   return do_attention(ctx, q, ld_q, n, cache_layer, is_new, score_partial, o, (cudaStream_t)stream, n);
 }
 
+// ---------------------------------------------------------------- cache of 8 bits, weights of 4
+namespace {
+
+constexpr int kScalePad = 64;
+
+bool quantized_shape(int batch, int seq_len, int n_kv_heads, int head_dim) {
+  return batch >= 1 && seq_len >= 1 && n_kv_heads >= 1 && (head_dim == 64 || head_dim == 80 || head_dim == 128);
+}
+
+inline int scale_pad(int seq_len) { return (int)(((int64_t)seq_len + kScalePad - 1) / kScalePad * kScalePad); }
+
+// Checks a caller's cache; what the kernels take of it.
+int quantized_cache(marche_ctx* ctx, const marche_quantized_cache* cache, QuantizedKv* kv) {
+  if (!cache || !cache->codes || !cache->scales) return MARCHE_EINVAL;
+  if (cache->batch < 1 || cache->seq_len < 1 || cache->n_kv_heads < 1) return MARCHE_EINVAL;
+  if (!quantized_shape(cache->batch, cache->seq_len, cache->n_kv_heads, cache->head_dim) || cache->seq_len > MARCHE_QUANTIZED_MAX_SEQ ||
+      (int64_t)cache->batch * cache->n_kv_heads * cache->head_dim > INT32_MAX / 2)
+    return MARCHE_ESHAPE;
+  if (((uintptr_t)cache->codes | (uintptr_t)cache->scales) & 15) return misaligned(ctx, "8-bit cache");
+  *kv = {cache->codes, cache->scales, cache->batch, cache->seq_len, cache->n_kv_heads, cache->head_dim, scale_pad(cache->seq_len)};
+  return MARCHE_OK;
+}
+
+// Rows that the copying kernels number with 32 bits.
+bool too_many_rows(const QuantizedKv& kv, int n) {
+  return (int64_t)kv.B * n * kv.H > INT32_MAX / (kv.dh / 16);
+}
+
+}  // namespace
+
+size_t marche_quantized_codes_bytes(int batch, int seq_len, int n_kv_heads, int head_dim) {
+  if (!quantized_shape(batch, seq_len, n_kv_heads, head_dim)) return 0;
+  return (size_t)2 * batch * seq_len * n_kv_heads * head_dim;
+}
+
+size_t marche_quantized_scales_bytes(int batch, int seq_len, int n_kv_heads, int head_dim) {
+  if (!quantized_shape(batch, seq_len, n_kv_heads, head_dim)) return 0;
+  return (size_t)2 * batch * n_kv_heads * scale_pad(seq_len) * sizeof(float);
+}
+
+int marche_scatter_kv_quantized(marche_ctx* ctx, const void* k, const void* v, int ld_kv, const int32_t* idx, int n,
+                                const marche_quantized_cache* cache, marche_stream stream) {
+  if (!ctx || !k || !v || n < 0) return MARCHE_EINVAL;
+  if (!ctx->bf16) return MARCHE_ESHAPE;
+  MARCHE_ENTER(ctx);
+  QuantizedKv kv;
+  const int rc = quantized_cache(ctx, cache, &kv);
+  if (rc) return rc;
+  if (ld_kv < kv.H * kv.dh || (!idx && n > kv.S)) return MARCHE_EINVAL;
+  if (too_many_rows(kv, n)) return MARCHE_ESHAPE;
+  if (ld_kv % 8 || (((uintptr_t)k | (uintptr_t)v) & 15)) return misaligned(ctx, "rows for an 8-bit cache");
+  if (n == 0) return MARCHE_OK;
+  mark(ctx, MARCHE_KC_SCATTER_KV, (cudaStream_t)stream);
+  MARCHE_TRY(launch_scatter_kv_quantized(k, v, ld_kv, idx, n, kv, (cudaStream_t)stream), "scatter_kv_quantized");
+  return MARCHE_OK;
+}
+
+int marche_gather_kv_quantized(marche_ctx* ctx, const marche_quantized_cache* cache, const int32_t* idx, int n, void* k_out,
+                               void* v_out, int ld_out, marche_stream stream) {
+  if (!ctx || !k_out || !v_out || n < 0) return MARCHE_EINVAL;
+  if (!ctx->bf16) return MARCHE_ESHAPE;
+  MARCHE_ENTER(ctx);
+  QuantizedKv kv;
+  const int rc = quantized_cache(ctx, cache, &kv);
+  if (rc) return rc;
+  if (ld_out < kv.H * kv.dh || (!idx && n > kv.S)) return MARCHE_EINVAL;
+  if (too_many_rows(kv, n)) return MARCHE_ESHAPE;
+  if (ld_out % 8 || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return misaligned(ctx, "rows of an 8-bit cache");
+  if (n == 0) return MARCHE_OK;
+  mark(ctx, MARCHE_KC_OTHER, (cudaStream_t)stream);
+  MARCHE_TRY(launch_gather_kv_quantized(kv, idx, n, k_out, v_out, ld_out, (cudaStream_t)stream), "gather_kv_quantized");
+  return MARCHE_OK;
+}
+
+int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, int n_heads, const marche_quantized_cache* cache,
+                               const int32_t* kv_len, void* o, marche_stream stream) {
+  if (!ctx || !q || !o || n < 0 || n_heads < 1) return MARCHE_EINVAL;
+  if (!ctx->bf16) return MARCHE_ESHAPE;
+  MARCHE_ENTER(ctx);
+  QuantizedKv kv;
+  const int rc = quantized_cache(ctx, cache, &kv);
+  if (rc) return rc;
+  if (n_heads % kv.H || (int64_t)n_heads * kv.dh > ld_q) return MARCHE_EINVAL;
+  // (rows of an item and CTAs of a launch are numbered with 32 bits)
+  if ((int64_t)n * (n_heads / kv.H) > (1 << 24) || (int64_t)kv.B * n * n_heads > INT32_MAX / 16) return MARCHE_ESHAPE;
+  if (ld_q % 8 || (((uintptr_t)q | (uintptr_t)o) & 15)) return misaligned(ctx, "attention over an 8-bit cache");
+  if (n == 0) return MARCHE_OK;
+  mark(ctx, MARCHE_KC_ATTENTION, (cudaStream_t)stream);
+  MARCHE_TRY(launch_attention_quantized(q, ld_q, n, n_heads, kv, kv_len, o, ctx->a_bf16, ctx->status_dev, (cudaStream_t)stream),
+             "attention_quantized");
+  return MARCHE_OK;
+}
+
+size_t marche_quantized_weights_bytes(int n, int k, int group, size_t* scales_bytes) {
+  const bool ok = n >= 16 && k >= 64 && n % 16 == 0 && k % 64 == 0 && (group == 32 || group == 64 || group == 128) && k % group == 0;
+  if (scales_bytes) *scales_bytes = ok ? (size_t)n * (k / group) * 2 : 0;
+  return ok ? (size_t)n * k / 2 : 0;
+}
+
+int marche_quantize_weights(marche_ctx* ctx, const float* w, const marche_quantized_weights* out, marche_stream stream) {
+  if (!ctx || !w || !out || !out->codes || !out->scales || out->n < 1 || out->k < 1 || out->group < 1) return MARCHE_EINVAL;
+  if (!ctx->bf16 || !marche_quantized_weights_bytes(out->n, out->k, out->group, nullptr) || out->k / 64 > 65535) return MARCHE_ESHAPE;
+  MARCHE_ENTER(ctx);
+  if (((uintptr_t)w | (uintptr_t)out->codes | (uintptr_t)out->scales) & 15) return misaligned(ctx, "weights of 4 bits");
+  mark(ctx, MARCHE_KC_OTHER, (cudaStream_t)stream);
+  MARCHE_TRY(launch_quantize_weights(w, out->n, out->k, out->group, out->codes, out->scales, (cudaStream_t)stream), "quantize_weights");
+  return MARCHE_OK;
+}
+
+int marche_linear_quantized(marche_ctx* ctx, const void* a, int lda, int M, const marche_quantized_weights* w, const float* bias, int epilogue,
+                            void* out, marche_stream stream) {
+  if (!ctx || !a || !w || !w->codes || !w->scales || !bias || !out || M < 0 || w->n < 1 || w->k < 1 || w->group < 1 || lda < w->k) return MARCHE_EINVAL;
+  if (epilogue < 0 || epilogue > 2) return MARCHE_EINVAL;
+  if (!ctx->bf16 || !marche_quantized_weights_bytes(w->n, w->k, w->group, nullptr) || M > MARCHE_QUANTIZED_MAX_ROWS) return MARCHE_ESHAPE;
+  MARCHE_ENTER(ctx);
+  if (lda % 8 || (((uintptr_t)a | (uintptr_t)w->codes | (uintptr_t)w->scales | (uintptr_t)bias | (uintptr_t)out) & 15)) return misaligned(ctx, "projection by weights of 4 bits");
+  if (M == 0) return MARCHE_OK;
+  mark(ctx, MARCHE_KC_OTHER, (cudaStream_t)stream);
+  MARCHE_TRY(launch_gemm_quantized(a, lda, M, w->codes, w->scales, bias, w->n, w->k, w->group, epilogue, out, ctx->a_bf16, (cudaStream_t)stream), "gemm_quantized");
+  return MARCHE_OK;
+}
+
 int marche_gather_rows(marche_ctx* ctx, const float* src, const int32_t* idx, int n, float* rows_out,
                        marche_stream stream) {
   if (!ctx || !src || !rows_out || n < 0 || n > ctx->cfg.seq_len || (n && !idx)) return MARCHE_EINVAL;

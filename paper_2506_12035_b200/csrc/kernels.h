@@ -158,6 +158,32 @@ cudaError_t launch_attention_twoseg(const void* qkv, int ld, int k_off, int v_of
                                     const int32_t* active_idx, void* cache_layer, const uint8_t* is_new,
                                     float* score_partial, void* o, bool o_bf16, int* status, cudaStream_t st);
 
+// One block's K and V held in 8 bits: codes [2][B][S][H * dh], scales [2][B][H][pad].
+struct QuantizedKv {
+  int8_t* codes;
+  float* scales;
+  int B, S, H, dh, pad;                    // H cached heads; pad: keys of a row of scales (S rounded up to 64)
+};
+
+// K7: rows of K and V (bf16 [B*n][ld]) into such a cache, and back.  idx NULL: tokens 0 .. n-1.  Rows whose token is not in 0 .. S-1 are left out.
+// B * n * H (and B * n * H * dh / 16) below 2^31; ld % 8 == 0, 16-byte aligned rows.
+cudaError_t launch_scatter_kv_quantized(const void* k, const void* v, int ld, const int32_t* idx, int n, const QuantizedKv& cache, cudaStream_t st);
+cudaError_t launch_gather_kv_quantized(const QuantizedKv& cache, const int32_t* idx, int n, void* k_out, void* v_out, int ld, cudaStream_t st);
+
+// K3 over such a cache: n query rows per sample, heads % cache.H == 0; kv_len [B] or NULL.  ld_q % 8 == 0, q 16-byte, o 8-byte aligned.
+// How a launch is cut: nr warps of 16 mt rows by nk groups along the key tiles in a CTA, nst stages for each group, n_rb blocks of rows, cs CTAs
+// along the keys.  R rows of an item (query rows that share a cached head).
+struct QuantizedSplit { int mt, nr, nk, nst, cs, n_rb; };
+QuantizedSplit attention_quantized_plan(int R, int S, int dh, int items);
+size_t attention_quantized_smem(int dh, const QuantizedSplit& s);
+cudaError_t launch_attention_quantized(const void* q, int ld_q, int n, int heads, const QuantizedKv& cache, const int32_t* kv_len, void* o,
+                                       bool o_bf16, int* status, cudaStream_t st);
+
+// K2 on weights of 4 bits.  N % 16 == 0, K % 64 == 0, group 32, 64 or 128 dividing K; lda % 8 == 0, 16-byte aligned operands.
+cudaError_t launch_gemm_quantized(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
+                                  int epilogue, void* out, bool a_bf16, cudaStream_t st);
+cudaError_t launch_quantize_weights(const float* w, int N, int K, int group, void* codes, void* scales, cudaStream_t st);
+
 // Diagnostic: one thread waits, with the library's bounded mbarrier wait, on a barrier nothing ever
 // arrives on; after limit_cycles it gives up, writes a code to *status and the kernel returns.
 cudaError_t launch_bounded_wait_probe(long long limit_cycles, int* status, cudaStream_t st);

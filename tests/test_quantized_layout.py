@@ -1,0 +1,71 @@
+"""Sizes and layouts of the 8-bit cache and the 4-bit weights as the library answers them, and what it refuses before it looks at a
+device (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+ESHAPE, EINVAL = -2, -1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2506_12035_b200 import binding, build
+    build.build()
+    return binding.load_library()
+
+
+@pytest.mark.parametrize("B,S,H,dh", [(1, 1, 1, 64), (2, 64, 12, 64), (3, 65, 16, 80), (128, 320, 16, 128), (2, 1 << 20, 8, 128)])
+def test_cache_sizes(lib, B, S, H, dh):
+    assert lib.marche_quantized_codes_bytes(B, S, H, dh) == 2 * B * S * H * dh
+    assert lib.marche_quantized_scales_bytes(B, S, H, dh) == 2 * B * H * ((S + 63) // 64 * 64) * 4
+
+
+@pytest.mark.parametrize("B,S,H,dh", [(0, 1, 1, 64), (1, 0, 1, 64), (1, 1, 0, 64), (1, 1, 1, 48), (1, 1, 1, 96), (-1, 1, 1, 64)])
+def test_cache_sizes_of_what_is_not_supported(lib, B, S, H, dh):
+    assert lib.marche_quantized_codes_bytes(B, S, H, dh) == 0 and lib.marche_quantized_scales_bytes(B, S, H, dh) == 0
+
+
+@pytest.mark.parametrize("n,k,group,ok", [(16, 64, 32, True), (16, 64, 64, True), (16, 64, 128, False), (768, 768, 128, True), (48, 192, 64, True),
+                                          (48, 192, 128, False), (8, 64, 64, False), (24, 64, 64, False), (16, 96, 32, False),
+                                          (16, 64, 16, False), (0, 64, 64, False), (16, 0, 64, False), (-16, 64, 64, False)])
+def test_weight_sizes(lib, n, k, group, ok):
+    scales = C.c_size_t(77)
+    got = lib.marche_quantized_weights_bytes(n, k, group, C.byref(scales))
+    assert got == (n * k // 2 if ok else 0) and scales.value == (n * (k // group) * 2 if ok else 0)
+    assert lib.marche_quantized_weights_bytes(n, k, group, None) == got
+
+
+def test_null_arguments(lib):
+    from paper_2506_12035_b200 import binding
+    cache, w = binding.MarcheQuantizedCache(), binding.MarcheQuantizedWeights()
+    p = 0x1000
+    assert lib.marche_scatter_kv_quantized(None, p, p, 64, None, 1, C.addressof(cache), None) == EINVAL
+    assert lib.marche_gather_kv_quantized(None, C.addressof(cache), None, 1, p, p, 64, None) == EINVAL
+    assert lib.marche_attention_quantized(None, p, 64, 1, 1, C.addressof(cache), None, p, None) == EINVAL
+    assert lib.marche_quantize_weights(None, p, C.addressof(w), None) == EINVAL
+    assert lib.marche_linear_quantized(None, p, 64, 1, C.addressof(w), p, 0, p, None) == EINVAL
+    assert C.sizeof(cache) == 32 and C.sizeof(w) == 32
+
+
+class Split(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("mt", "nr", "nk", "nst", "cs", "n_rb")]
+
+
+def test_attention_cuts_fit_an_sm_and_cover_all_rows(lib):
+    """Every way in which a launch is cut keeps to the shared memory, the barriers and the warps of a CTA, and covers the rows."""
+    plan, smem = lib._ZN6marche24attention_quantized_planEiiii, lib._ZN6marche24attention_quantized_smemEiRKNS_14QuantizedSplitE
+    plan.restype, plan.argtypes = Split, [C.c_int] * 4
+    smem.restype, smem.argtypes = C.c_size_t, [C.c_int, C.POINTER(Split)]
+    rows = list(range(1, 34)) + [48, 49, 64, 65, 80, 96, 97, 127, 128, 129, 160, 256, 257, 300, 1000, 5000, 1 << 20]
+    for dh in (64, 80, 128):
+        for R in rows:
+            for S in (1, 2, 63, 64, 65, 128, 129, 192, 200, 256, 257, 320, 321, 512, 576, 700, 1088, 2048, 5000, 65521, 1 << 24):
+                for items in (1, 2, 8, 12, 24, 32, 60, 74, 75, 148, 149, 300, 592, 900, 2048):
+                    s = plan(R, S, dh, items)
+                    at = (dh, R, S, items, [getattr(s, n) for n, _ in Split._fields_])
+                    assert s.mt in (1, 2) and s.nr >= 1 and s.nk >= 1 and s.nst >= 1 and s.cs in (1, 2, 4, 8), at
+                    assert s.nr * s.nk <= 8 and s.nk * s.nst <= 16 and smem(dh, C.byref(s)) <= 226 * 1024, at
+                    assert s.n_rb * s.nr * 16 * s.mt >= R and (s.n_rb - 1) * s.nr * 16 * s.mt < R, at
+                    tiles = (S + 63) // 64
+                    mine = -(-(-(-tiles // s.cs)) // s.nk)
+                    assert s.nst >= min(mine, 3 if s.nr > 1 else 2), at            # a stage is filled again one tile late
