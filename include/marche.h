@@ -491,7 +491,7 @@ int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, 
  *           multiplies: [n/16][k/64][lane 0..31][word 0..3], little-endian words of eight nibbles code + 8.
  *           With g = lane / 4, t = lane % 4, nibble i of word s (i = r + 4 e, r = 0..3, e = 0, 1; bits 4 r + 16 e up)
  *           holds output 16 tile + g + 8 (r % 2), input 64 chunk + 32 (s / 2) + 8 t + 4 (s % 2) + 2 (r / 2) + e.
- *   scales  bf16 [n/16][k/group][16]; *scales_bytes receives their size
+ *   scales  bf16 [n/16][k/group][16], outputs 0, 8, 1, 9, .. 7, 15 of a tile; *scales_bytes receives their size
  * Both 16-byte aligned. */
 typedef struct {
   void* codes;

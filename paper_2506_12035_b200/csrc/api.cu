@@ -963,7 +963,7 @@ int marche_linear_quantized(marche_ctx* ctx, const void* a, int lda, int M, cons
   if (lda % 8 || (((uintptr_t)a | (uintptr_t)w->codes | (uintptr_t)w->scales | (uintptr_t)bias | (uintptr_t)out) & 15)) return misaligned(ctx, "projection by weights of 4 bits");
   if (M == 0) return MARCHE_OK;
   mark(ctx, MARCHE_KC_OTHER, (cudaStream_t)stream);
-  MARCHE_TRY(launch_gemm_quantized(a, lda, M, w->codes, w->scales, bias, w->n, w->k, w->group, epilogue, out, ctx->a_bf16, (cudaStream_t)stream), "gemm_quantized");
+  MARCHE_TRY(launch_gemm_quantized(a, lda, M, w->codes, w->scales, bias, w->n, w->k, w->group, epilogue, out, ctx->a_bf16, ctx->status_dev, (cudaStream_t)stream), "gemm_quantized");
   return MARCHE_OK;
 }
 

@@ -14,6 +14,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "launch_pdl.h"
+#include "sm100_ptx.cuh"
 #include "tma_host.h"
 
 namespace marche {
@@ -26,11 +27,22 @@ constexpr int kMaxRows = 32;               // of a CTA
 template <bool BF>
 MARCHE_DEVINL void mma_weights(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if (BF)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// The same into a fresh accumulator.
+template <bool BF>
+MARCHE_DEVINL void mma_weights_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (BF)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // (w & mask) | magic in one instruction
@@ -68,44 +80,82 @@ MARCHE_DEVINL uint4 ld_stream(const uint4* p) {
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+// Two neighbouring outputs n, n + 1 of a row: bias, epilogue, store.
+MARCHE_DEVINL void finish(float2 y, const float* __restrict__ bias, int row, int n, int N, int epi, void* __restrict__ out, int out_bf16) {
+  const float2 b = __ldg(reinterpret_cast<const float2*>(bias + n));
+  const size_t at = (size_t)row * N + n;
+  y.x += b.x;
+  y.y += b.y;
+  if (epi == 1) {
+    float2* o = reinterpret_cast<float2*>((float*)out + at);
+    const float2 r = *o;
+    *o = make_float2(r.x + y.x, r.y + y.y);
+  } else {
+    if (epi == 2) { y.x = gelu_erf(y.x); y.y = gelu_erf(y.y); }
+    reinterpret_cast<uint32_t*>(out)[at >> 1] = pack_a16x2(y.x, y.y, out_bf16 != 0);
+  }
+}
 
-// blockIdx.x: NT tiles of 16 outputs; blockIdx.y: 8 MT rows.  The CTA's warps take the 64-wide chunks of K in turn, PF chunks ahead of
-// themselves.  G32: k16 steps of a group of 32 inputs (2), else a group is one or two whole chunks.
-template <int NT, int MT, bool BF, bool G32>
-__global__ void __launch_bounds__(NT == 1 ? 512 : 256)
-gemm_quantized_kernel(const uint16_t* __restrict__ a, int lda, int M, const uint4* __restrict__ codes, const uint16_t* __restrict__ scales,
-                      const float* __restrict__ bias, int N, int K, int group, int epi, void* __restrict__ out, int out_bf16) {
-  constexpr int PF = NT == 1 ? 4 : 3;
-  extern __shared__ float parts[];                         // [warp][8 MT rows][16 NT outputs]
+// A chunk of a tile (a lane's 16 bytes of codes; G / 32 groups, or part of one) times 8 MT rows (a lane's 16 values of each eight), scaled and added up.
+// both(k): scales of the chunk's k-th group for outputs g and g + 8.
+template <int MT, bool BF, int G, typename Both>
+MARCHE_DEVINL void multiply_chunk(float (&acc)[MT][4], const uint4& w, const uint4 (&x)[MT][2], Both both) {
+  const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+  float part[MT][4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    uint32_t f[4];
+    numbers_of<BF>(words[s], f);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const uint4& v = x[m][s >> 1];
+      if (s == 0 || (G == 32 && s == 2)) mma_weights_first<BF>(part[m], f, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
+      else mma_weights<BF>(part[m], f, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
+    }
+    if (s == 3 || (G == 32 && s == 1)) {
+      const uint32_t sc = both(s >> 1);
+      const float s0 = __uint_as_float(sc << 16), s1 = __uint_as_float(sc & 0xffff0000u);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        acc[m][0] = fmaf(part[m][0], s0, acc[m][0]);
+        acc[m][1] = fmaf(part[m][1], s0, acc[m][1]);
+        acc[m][2] = fmaf(part[m][2], s1, acc[m][2]);
+        acc[m][3] = fmaf(part[m][3], s1, acc[m][3]);
+      }
+    }
+  }
+}
+
+// Small matrices: a CTA per tile of 16 outputs and 8 MT rows, whose warps take the chunks of K in turn, straight from global memory to registers
+// PF chunks ahead; the first of them before the dependency wait.
+template <int MT, bool BF, int G>
+__global__ void __launch_bounds__(512)
+gemm_quantized_small_kernel(const uint16_t* __restrict__ a, int lda, int M, const uint4* __restrict__ codes, const uint32_t* __restrict__ scales,
+                            const float* __restrict__ bias, int N, int K, int epi, void* __restrict__ out, int out_bf16) {
+  constexpr int PF = 4, SC = G == 32 ? 2 : 1;
+  extern __shared__ float sums[];                          // [warp][8 MT rows][16]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
-  const int chunks = K / kChunk, tile0 = blockIdx.x * NT, tiles = N / 16, row0 = blockIdx.y * (8 * MT);
-  const int n_groups = K / group;
-  const uint4* src[NT];
-  const uint16_t* sc[NT];
+  const int chunks = K / kChunk, row0 = blockIdx.y * (8 * MT);
+  const uint4* src = codes + (size_t)blockIdx.x * chunks * 32 + lane;
+  const uint32_t* sc = scales + (size_t)blockIdx.x * (K / G) * 8 + g;
+  uint4 w[PF];
+  uint32_t ws[PF][SC];
+  auto fetch = [&](int p, int c) {
+    w[p] = ld_stream(src + (size_t)c * 32);
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int tile = min(tile0 + i, tiles - 1);            // (the last CTA's surplus tile is computed and not stored)
-    src[i] = codes + (size_t)tile * chunks * 32 + lane;
-    sc[i] = scales + (size_t)tile * n_groups * 16 + g;
-  }
-  uint4 w[PF][NT];
+    for (int k = 0; k < SC; ++k) ws[p][k] = __ldg(sc + (size_t)(G == 32 ? 2 * c + k : c * kChunk / G) * 8);
+  };
 #pragma unroll
-  for (int p = 0; p < PF; ++p) {
-    const int c = warp + p * warps;
-#pragma unroll
-    for (int i = 0; i < NT; ++i) w[p][i] = c < chunks ? ld_stream(src[i] + (size_t)c * 32) : make_uint4(0, 0, 0, 0);
-  }
+  for (int p = 0; p < PF; ++p)
+    if (warp + p * warps < chunks) fetch(p, warp + p * warps);
   pdl_sync();                                              // the weights are on their way while the previous kernel drains
 
-  float acc[NT][MT][4];
+  float acc[MT][4];
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
+  for (int m = 0; m < MT; ++m) acc[m][0] = acc[m][1] = acc[m][2] = acc[m][3] = 0.f;
+  const uint4* row[MT];                                    // (rows behind the last are the last one again: what they give is not stored)
 #pragma unroll
-    for (int m = 0; m < MT; ++m) acc[i][m][0] = acc[i][m][1] = acc[i][m][2] = acc[i][m][3] = 0.f;
-  const uint16_t* rows[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) rows[m] = a + (size_t)(row0 + 8 * m + g) * lda + 8 * t;
-
+  for (int m = 0; m < MT; ++m) row[m] = reinterpret_cast<const uint4*>(a + (size_t)min(row0 + 8 * m + g, M - 1) * lda + 8 * t);
   for (int c0 = warp; c0 < chunks; c0 += PF * warps) {
 #pragma unroll
     for (int p = 0; p < PF; ++p) {
@@ -113,72 +163,185 @@ gemm_quantized_kernel(const uint16_t* __restrict__ a, int lda, int M, const uint
       if (c < chunks) {
         uint4 x[MT][2];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-            x[m][hf] = row0 + 8 * m + g < M ? *reinterpret_cast<const uint4*>(rows[m] + (size_t)c * kChunk + 32 * hf) : make_uint4(0, 0, 0, 0);
-        const int next = c + PF * warps;
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const uint32_t words[4] = {w[p][i].x, w[p][i].y, w[p][i].z, w[p][i].w};
-          float part[MT][4];
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            if (s == 0 || (G32 && s == 2)) {
-#pragma unroll
-              for (int m = 0; m < MT; ++m) part[m][0] = part[m][1] = part[m][2] = part[m][3] = 0.f;
-            }
-            uint32_t f[4];
-            numbers_of<BF>(words[s], f);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-              const uint4& v = x[m][s >> 1];
-              mma_weights<BF>(part[m], f, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
-            }
-            if (s == 3 || (G32 && s == 1)) {
-              const uint16_t* at = sc[i] + (size_t)(G32 ? 2 * c + (s >> 1) : c * kChunk / group) * 16;
-              const float s0 = __uint_as_float((uint32_t)__ldg(at) << 16), s1 = __uint_as_float((uint32_t)__ldg(at + 8) << 16);
-#pragma unroll
-              for (int m = 0; m < MT; ++m) {
-                acc[i][m][0] = fmaf(part[m][0], s0, acc[i][m][0]);
-                acc[i][m][1] = fmaf(part[m][1], s0, acc[i][m][1]);
-                acc[i][m][2] = fmaf(part[m][2], s1, acc[i][m][2]);
-                acc[i][m][3] = fmaf(part[m][3], s1, acc[i][m][3]);
-              }
-            }
-          }
-          if (next < chunks) w[p][i] = ld_stream(src[i] + (size_t)next * 32);
+        for (int m = 0; m < MT; ++m) {
+          x[m][0] = row[m][c * 8];
+          x[m][1] = row[m][c * 8 + 4];
         }
+        multiply_chunk<MT, BF, G>(acc, w[p], x, [&](int k) { return ws[p][G == 32 ? k : 0]; });
+        if (c + PF * warps < chunks) fetch(p, c + PF * warps);
       }
     }
   }
   // accumulator: outputs g and g + 8, rows 2 t and 2 t + 1 of an eight
-  float* mine = parts + warp * (8 * MT * 16 * NT);
+  float* mine = sums + warp * (8 * MT * 16);
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
+  for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * (16 * NT) + 16 * i + g + 8 * (e >> 1)] = acc[i][m][e];
+    for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * 16 + g + 8 * (e >> 1)] = acc[m][e];
   __syncthreads();
-  for (int q = threadIdx.x; q < 8 * MT * 8 * NT; q += blockDim.x) {      // two neighbouring outputs
-    const int m = q / (8 * NT), col = 2 * (q - m * (8 * NT)), row = row0 + m, n = tile0 * 16 + col;
-    if (row >= M || n >= N) continue;
-    float2 y = __ldg(reinterpret_cast<const float2*>(bias + n));
-    for (int k = 0; k < warps; ++k) {
-      const float2 v = *reinterpret_cast<const float2*>(parts + k * (8 * MT * 16 * NT) + m * (16 * NT) + col);
+  const int all = min(8 * MT, M - row0) * 8;               // two neighbouring outputs of a row each
+  for (int q = threadIdx.x; q < all; q += blockDim.x) {
+    float2 y = make_float2(0.f, 0.f);
+    for (int k = 0; k < warps; ++k) {                      // over the warps, in their order
+      const float2 v = *reinterpret_cast<const float2*>(sums + k * (8 * MT * 16) + 2 * q);
       y.x += v.x;
       y.y += v.y;
     }
-    if (epi == 1) {
-      float2* o = reinterpret_cast<float2*>((float*)out + (size_t)row * N + n);
-      const float2 r = *o;
-      *o = make_float2(r.x + y.x, r.y + y.y);
-    } else {
-      if (epi == 2) { y.x = gelu_erf(y.x); y.y = gelu_erf(y.y); }
-      reinterpret_cast<uint32_t*>(out)[((size_t)row * N + n) >> 1] = pack_a16x2(y.x, y.y, out_bf16 != 0);
+    finish(y, bias, row0 + (q >> 3), blockIdx.x * 16 + 2 * (q & 7), N, epi, out, out_bf16);
+  }
+}
+
+constexpr int kMaxStages = 16;
+constexpr int WK = 2;                      // warps that share tiles and split K
+enum { ST_GEMM_QUANTIZED = 0x66 };
+
+// Of a stage: 2 CW chunks of the rows (a chunk's 128 bytes under TMA's 128-byte swizzle, eight rows 1 KB), of the unit's tiles, and their scales.
+template <int MT, int CW, int G> struct Stage {
+  static constexpr int CHUNKS = WK * CW, GROUPS = CHUNKS * kChunk / G, ROWS = CHUNKS * MT * 1024, CODES = CHUNKS * 512, SCALES = GROUPS * 32;
+  static_assert(CHUNKS * kChunk % G == 0, "whole groups");
+};
+inline size_t stage_bytes_of(int mt, int cw, int group, int tiles) {
+  const size_t codes = (size_t)tiles * WK * cw * 512, scales = (size_t)tiles * (WK * cw * kChunk / group) * 32;
+  return ((size_t)WK * cw * mt * 1024 + codes + scales + 1023) / 1024 * 1024;
+}
+
+// Large matrices: persistent CTAs, one per SM.  A unit is wn * NT tiles of 16 outputs by 8 MT rows, units are dealt in turn; warp (iw, ik) has NT
+// of the tiles and every second group of CW chunks.  Codes, scales and rows of a stage come by one TMA box each (bulk copies of a tile's or a
+// row's part alone take 40 ns apiece: 31 x 24576 x 12288 211 us for the copies) into a ring that all warps share and that a warp of its own fills, over
+// the borders of units, too: the matrix flows in without a pause, and a row is read from L2 once per unit.  (A consumer that fills slots on the
+// way, with divisions for the slot and its phase, took 860 cycles for every stage, whatever it loaded.)
+template <int NT, int MT, int CW, bool BF, int G>
+__global__ void __launch_bounds__(NT <= 2 ? 480 : 288)
+gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_codes,
+                             const __grid_constant__ CUtensorMap tmap_scales, int M, const float* __restrict__ bias, int N, int K, int epi,
+                             void* __restrict__ out, int out_bf16, int wn, int nst, uint32_t stage_bytes, int* __restrict__ status) {
+  using St = Stage<MT, CW, G>;
+  extern __shared__ uint8_t smem_raw[];                    // stages (1 KB aligned): [chunk][rows] | [tile][chunk] codes | [tile][group] scales; sums [WK][8 MT rows][cols]
+  __shared__ __align__(8) uint64_t bars[2 * kMaxStages];   // full, empty
+  __shared__ int abort_flags[2];
+  volatile int* abort_flag = abort_flags;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, iw = warp >> 1, ik = warp & 1, g = lane >> 2, t = lane & 3;
+  const int chunks = K / kChunk, tiles = N / 16, tiles_unit = NT * wn, cols = 16 * tiles_unit, n_rb = (M + 8 * MT - 1) / (8 * MT);
+  const int units = (tiles + tiles_unit - 1) / tiles_unit * n_rb, per_unit = (chunks + St::CHUNKS - 1) / St::CHUNKS;
+  const uint32_t scales_at = (uint32_t)(St::ROWS + tiles_unit * St::CODES), filling = scales_at + (uint32_t)(tiles_unit * St::SCALES);
+  const uint32_t raw = ptx::smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u, full0 = ptx::smem_u32(bars), empty0 = full0 + 8u * kMaxStages;
+  const uint8_t* smem = smem_raw + (ring - raw);
+  float* sums = reinterpret_cast<float*>(smem_raw + (ring - raw) + (size_t)nst * stage_bytes);
+
+  if (threadIdx.x == 0) {
+    abort_flags[0] = abort_flags[1] = 0;
+    for (int i = 0; i < nst; ++i) {
+      ptx::mbar_init(full0 + 8u * i, 1);
+      ptx::mbar_init(empty0 + 8u * i, 2 * wn);
+    }
+    ptx::fence_barrier_init();
+    ptx::prefetch_tensormap(&tmap_codes);
+    ptx::prefetch_tensormap(&tmap_scales);
+    ptx::prefetch_tensormap(&tmap_a);
+  }
+  __syncthreads();
+  bool ok = true;
+  if (warp == 2 * wn) {
+    // ---------------------------------------------------------------- producer (what lies outside the matrices comes as zeros)
+    if (ptx::elect_one()) {
+      // codes and scales, which no kernel writes, and rows, apart so that the first ones' codes can go ahead of the dependency wait
+      auto load_codes = [&](int slot, int tile0, int piece) {
+        const uint32_t dst = ring + (uint32_t)slot * stage_bytes, bar = full0 + 8u * slot;
+        ptx::mbar_expect_tx(bar, filling);
+        ptx::tma_load_3d(dst + St::ROWS, &tmap_codes, 0, piece * St::CHUNKS, tile0, bar);
+        ptx::tma_load_3d(dst + scales_at, &tmap_scales, 0, piece * St::GROUPS, tile0, bar);
+      };
+      auto load_rows = [&](int slot, int row0, int piece) {
+        ptx::tma_load_3d(ring + (uint32_t)slot * stage_bytes, &tmap_a, 0, row0, piece * St::CHUNKS, full0 + 8u * slot);
+      };
+      const int ahead = min(nst, per_unit);                // of the first unit's
+      {
+        const int tile0 = (int)blockIdx.x / n_rb * tiles_unit, row0 = (int)blockIdx.x % n_rb * (8 * MT);
+        for (int i = 0; i < ahead; ++i) load_codes(i, tile0, i);
+        pdl_wait();
+        for (int i = 0; i < ahead; ++i) load_rows(i, row0, i);
+      }
+      int slot = ahead == nst ? 0 : ahead, phase = ahead == nst ? 0 : 1, filled = ahead;   // phase: parity of the emptying waited for (1: a fresh slot passes)
+      for (int unit = blockIdx.x, first = ahead; unit < units && ok; unit += gridDim.x, first = 0) {
+        const int tile0 = unit / n_rb * tiles_unit, row0 = unit % n_rb * (8 * MT);
+        for (int p = first; p < per_unit; ++p) {
+          if (!ptx::mbar_wait(empty0 + 8u * slot, (uint32_t)phase, abort_flag)) { ok = false; break; }
+          load_codes(slot, tile0, p);
+          load_rows(slot, row0, p);
+          ++filled;
+          if (++slot == nst) { slot = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {                                           // let copies already issued land before the CTA's shared memory is released
+        *(volatile int*)status = ST_GEMM_QUANTIZED;
+        for (int k = filled > nst ? filled - nst : 0; k < filled; ++k)
+          ptx::mbar_wait(full0 + 8u * (k % nst), (uint32_t)(k / nst) & 1u, abort_flag + 1, 20000000LL);
+      }
+    }
+    __syncwarp();
+    pdl_launch_dependents();
+    return;
+  }
+  pdl_sync();
+  const int consumers = 64 * wn;                           // (their barriers do not wait for the producer, which runs ahead)
+  auto sync_consumers = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(consumers) : "memory"); };
+
+  const uint32_t x_lo = (uint32_t)(g * 128 + ((t ^ g) << 4)), x_hi = x_lo ^ 64u;   // a lane's pieces of a row, swizzled
+  int slot = 0, phase = 0;
+  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int row0 = (unit % n_rb) * (8 * MT), col0 = unit / n_rb * cols;
+    float acc[NT][MT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[i][m][0] = acc[i][m][1] = acc[i][m][2] = acc[i][m][3] = 0.f;
+    for (int p = 0; p < per_unit && ok; ++p) {
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8u * slot, (uint32_t)phase, abort_flag))) { ok = false; break; }
+      const uint8_t* stage = smem + (uint32_t)slot * stage_bytes;
+      const uint8_t* w_at = stage + St::ROWS + iw * NT * St::CODES + lane * 16;
+      const uint8_t* s_at = stage + scales_at + iw * NT * St::SCALES + g * 4;
+      const int left = chunks - p * St::CHUNKS;
+#pragma unroll
+      for (int j = 0; j < CW; ++j) {
+        const int c = ik * CW + j;                         // of the stage
+        if (c < left) {
+          uint4 x[MT][2];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            x[m][0] = *reinterpret_cast<const uint4*>(stage + x_lo + (c * MT + m) * 1024);
+            x[m][1] = *reinterpret_cast<const uint4*>(stage + x_hi + (c * MT + m) * 1024);
+          }
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+            multiply_chunk<MT, BF, G>(acc[i], *reinterpret_cast<const uint4*>(w_at + i * St::CODES + c * 512), x, [&](int k) {
+              return *reinterpret_cast<const uint32_t*>(s_at + i * St::SCALES + (G == 32 ? 2 * c + k : c * kChunk / G) * 32);
+            });
+        }
+      }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(empty0 + 8u * slot);
+      if (++slot == nst) { slot = 0; phase ^= 1; }
+    }
+    // accumulator: outputs g and g + 8, rows 2 t and 2 t + 1 of an eight
+    sync_consumers();                                      // the unit before has been stored
+    float* mine = sums + ik * (8 * MT * cols) + 16 * NT * iw;
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * cols + 16 * i + g + 8 * (e >> 1)] = acc[i][m][e];
+    sync_consumers();
+    if (*abort_flag) { ok = false; continue; }             // nothing is stored of what is missing; the barriers stay in step
+    const int pairs = cols / 2, all = min(8 * MT, M - row0) * pairs;   // two neighbouring outputs of a row each
+    for (int q = threadIdx.x; q < all; q += consumers) {
+      const int m = q / pairs, n = col0 + 2 * (q - m * pairs);
+      if (n >= N) continue;
+      const float2 u = *reinterpret_cast<const float2*>(sums + 2 * q), v = *reinterpret_cast<const float2*>(sums + 8 * MT * cols + 2 * q);
+      finish(make_float2(u.x + v.x, u.y + v.y), bias, row0 + m, n, N, epi, out, out_bf16);
     }
   }
+  if (!ok && lane == 0) *(volatile int*)status = ST_GEMM_QUANTIZED;
 }
 
 // One CTA per tile of 16 outputs and span of max(64, group) inputs: eight threads per output find the scales, then every thread packs words.
@@ -202,7 +365,7 @@ quantize_weights_kernel(const float* __restrict__ w, int N, int K, int group, ui
   if (j * per % group == 0) {
     const int in_span = j * per / group;
     s_scale[r][in_span] = __bfloat162float(rounded);
-    scales[((size_t)tile * (K / group) + k0 / group + in_span) * 16 + r] = __bfloat16_as_ushort(rounded);
+    scales[((size_t)tile * (K / group) + k0 / group + in_span) * 16 + 2 * (r & 7) + (r >> 3)] = __bfloat16_as_ushort(rounded);
   }
   __syncthreads();
   for (int q = threadIdx.x; q < span / kChunk * 128; q += 128) {
@@ -220,56 +383,108 @@ quantize_weights_kernel(const float* __restrict__ w, int N, int K, int group, ui
   }
 }
 
-struct Shape { int nt, warps; };
+}  // namespace
 
-// Tiles of a warp and warps of a CTA.  Two tiles share what is read of the rows, one gives twice the CTAs.
-Shape pick(int M, int N, int K) {
-  const int tiles = N / 16, chunks = K / kChunk, sms = device_sm_count();
-  Shape s;
-  s.nt = tiles >= 4 * sms ? 2 : 1;
-  s.warps = chunks < 8 ? chunks : 8;
-  const int ctas = (tiles + s.nt - 1) / s.nt;
-  if (ctas <= sms) s.warps = chunks < 16 ? chunks : 16;
+// How a projection is cut.  stream false: warps of a CTA of the kernel for small matrices.  Else tiles of a warp, warps along the outputs, stages.
+QuantizedGemmShape gemm_quantized_pick(int M, int N, int K, int group) {
+  const int tiles = N / 16, chunks = K / kChunk, sms = device_sm_count(), mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
+  QuantizedGemmShape s = {};
+  s.stream = tiles >= 2 * sms && (long)tiles * chunks >= 64L * sms;
+  if (!s.stream) {
+    s.warps = chunks < 8 ? chunks : (tiles <= sms && chunks >= 16 ? 16 : 8);
+    return s;
+  }
+  // the fewest tiles in turn on an SM
+  long best = 0;
+  for (int nt = 1; nt <= (mt >= 3 ? 3 : 1); ++nt)
+    for (int wn = 4; wn <= (nt <= 2 ? 7 : 4); ++wn) {
+      const long cost = ((tiles + nt * wn - 1) / (nt * wn) + sms - 1) / sms * nt * wn;
+      if (!best || cost <= best) { best = cost; s.nt = nt; s.wn = wn; }
+    }
+  s.cw = mt == 1 ? 4 : (mt == 2 ? 2 : 1);
+  s.nst = 1;
+  while (s.nst < kMaxStages) {
+    ++s.nst;
+    if (gemm_quantized_smem(M, group, s) > 200 * 1024) { --s.nst; break; }
+  }
   return s;
 }
 
-template <int NT, int MT, bool BF, bool G32>
-cudaError_t launch(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group, int epi,
-                   void* out, int out_bf16, int warps, cudaStream_t st) {
-  const size_t smem = (size_t)warps * (8 * MT * 16 * NT) * 4;
+size_t gemm_quantized_smem(int M, int group, const QuantizedGemmShape& s) {
+  const int mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
+  if (!s.stream) return (size_t)s.warps * 8 * mt * 16 * 4;
+  const int tiles = s.nt * s.wn;
+  return 1024 + (size_t)s.nst * stage_bytes_of(mt, s.cw, group, tiles) + (size_t)WK * 8 * mt * 16 * tiles * 4;
+}
+
+namespace {
+
+struct Args {
+  const void* a; int lda, M; const void* codes; const void* scales; const float* bias; int N, K, group, epi; void* out; int out_bf16, *status; cudaStream_t st;
+};
+
+template <int MT, bool BF, int G>
+cudaError_t launch_small(const Args& p, const QuantizedGemmShape& s) {
+  return launch_pdl(gemm_quantized_small_kernel<MT, BF, G>, dim3(p.N / 16, (p.M + 8 * MT - 1) / (8 * MT)), dim3(32 * s.warps), gemm_quantized_smem(p.M, G, s), p.st,
+                    (const uint16_t*)p.a, p.lda, p.M, (const uint4*)p.codes, (const uint32_t*)p.scales, p.bias, p.N, p.K, p.epi, p.out, p.out_bf16);
+}
+
+template <int NT, int MT, int CW, bool BF, int G>
+cudaError_t launch_stream(const Args& p, const QuantizedGemmShape& s) {
+  const size_t smem = gemm_quantized_smem(p.M, G, s);
+  if (smem > 220 * 1024 || s.nst < 2 || s.wn * WK > (NT <= 2 ? 14 : 8) || s.cw != CW || s.nt != NT) return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
-  cudaError_t e = smem > 48 * 1024 ? ensure_dynamic_smem(gemm_quantized_kernel<NT, MT, BF, G32>, smem, smem_set) : cudaSuccess;
+  cudaError_t e = ensure_dynamic_smem(gemm_quantized_stream_kernel<NT, MT, CW, BF, G>, smem, smem_set);
   if (e != cudaSuccess) return e;
-  return launch_pdl(gemm_quantized_kernel<NT, MT, BF, G32>, dim3((N / 16 + NT - 1) / NT, (M + 8 * MT - 1) / (8 * MT)), dim3(32 * warps), smem, st,
-                    (const uint16_t*)a, lda, M, (const uint4*)codes, (const uint16_t*)scales, bias, N, K, group, epi, out, out_bf16);
+  const int per = NT * s.wn, sms = device_sm_count();
+  const long units = (long)((p.N / 16 + per - 1) / per) * ((p.M + 8 * MT - 1) / (8 * MT));
+  // boxes of a stage: [chunk][8 MT rows][64 values], [tile][chunk][512 bytes], [tile][group][32 bytes]
+  using St = Stage<MT, CW, G>;
+  CUtensorMap ta, tc, ts;
+  EncodeTiledFn fn = tma_encode_fn();
+  const cuuint64_t chunks = p.K / kChunk, groups = p.K / G, tiles = p.N / 16;
+  auto make = [&](CUtensorMap* map, CUtensorMapDataType type, const void* ptr, cuuint64_t d0, cuuint64_t d1, cuuint64_t d2, cuuint64_t s1, cuuint64_t s2, int b0,
+                  int b1, int b2, bool swizzle) {
+    const cuuint64_t dims[3] = {d0, d1, d2}, strides[2] = {s1, s2};
+    const cuuint32_t box[3] = {(cuuint32_t)b0, (cuuint32_t)b1, (cuuint32_t)b2}, unit[3] = {1, 1, 1};
+    return fn && fn(map, type, 3, const_cast<void*>(ptr), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (!make(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.a, kChunk, p.M, chunks, (cuuint64_t)p.lda * 2, kChunk * 2, kChunk, 8 * MT, St::CHUNKS, true) ||
+      !make(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.codes, 128, chunks, tiles, 512, chunks * 512, 128, St::CHUNKS, per, false) ||
+      !make(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.scales, 8, groups, tiles, 32, groups * 32, 8, St::GROUPS, per, false))
+    return cudaErrorInvalidValue;
+  return launch_pdl(gemm_quantized_stream_kernel<NT, MT, CW, BF, G>, dim3((unsigned)(units < sms ? units : sms)), dim3(32 * (s.wn * WK + 1)), smem, p.st, ta, tc, ts, p.M, p.bias,
+                    p.N, p.K, p.epi, p.out, p.out_bf16, s.wn, s.nst, (uint32_t)stage_bytes_of(MT, CW, G, per), p.status);
+}
+
+template <bool BF, int G>
+cudaError_t launch(const Args& p, const QuantizedGemmShape& s, int mt) {
+  if (!s.stream) {
+    switch (mt) {
+      case 1: return launch_small<1, BF, G>(p, s);
+      case 2: return launch_small<2, BF, G>(p, s);
+      case 3: return launch_small<3, BF, G>(p, s);
+      default: return launch_small<4, BF, G>(p, s);
+    }
+  }
+  if (mt == 1) return launch_stream<1, 1, 4, BF, G>(p, s);
+  if (mt == 2) return launch_stream<1, 2, 2, BF, G>(p, s);
+  if (mt == 3) return s.nt == 2 ? launch_stream<2, 3, 1, BF, G>(p, s) : s.nt == 1 ? launch_stream<1, 3, 1, BF, G>(p, s) : launch_stream<3, 3, 1, BF, G>(p, s);
+  return s.nt == 2 ? launch_stream<2, 4, 1, BF, G>(p, s) : s.nt == 1 ? launch_stream<1, 4, 1, BF, G>(p, s) : launch_stream<3, 4, 1, BF, G>(p, s);
 }
 
 }  // namespace
 
 cudaError_t launch_gemm_quantized(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
-                                  int epilogue, void* out, bool a_bf16, cudaStream_t st) {
-  const Shape s = pick(M, N, K);
-  const int mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8, ob = epilogue == 0 || a_bf16;   // (the bias epilogue's output is bf16)
-#define MARCHE_Q_LAUNCH(NT_, MT_, BF_, G_) \
-  return launch<NT_, MT_, BF_, G_>(a, lda, M, codes, scales, bias, N, K, group, epilogue, out, ob, s.warps, st)
-#define MARCHE_Q_TYPE(NT_, MT_)                                                     \
-  do {                                                                              \
-    if (a_bf16) { if (group == 32) MARCHE_Q_LAUNCH(NT_, MT_, true, true); MARCHE_Q_LAUNCH(NT_, MT_, true, false); } \
-    if (group == 32) MARCHE_Q_LAUNCH(NT_, MT_, false, true);                        \
-    MARCHE_Q_LAUNCH(NT_, MT_, false, false);                                        \
-  } while (0)
-#define MARCHE_Q_ROWS(NT_)                     \
-  do {                                         \
-    if (mt == 1) MARCHE_Q_TYPE(NT_, 1);        \
-    if (mt == 2) MARCHE_Q_TYPE(NT_, 2);        \
-    if (mt == 3) MARCHE_Q_TYPE(NT_, 3);        \
-    MARCHE_Q_TYPE(NT_, 4);                     \
-  } while (0)
-  if (s.nt == 2) MARCHE_Q_ROWS(2);
-  MARCHE_Q_ROWS(1);
-#undef MARCHE_Q_ROWS
-#undef MARCHE_Q_TYPE
-#undef MARCHE_Q_LAUNCH
+                                  int epilogue, void* out, bool a_bf16, int* status, cudaStream_t st) {
+  const QuantizedGemmShape s = gemm_quantized_pick(M, N, K, group);
+  const int mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
+  // (the bias epilogue's output is bf16 in every 16-bit context)
+  const Args p = {a, lda, M, codes, scales, bias, N, K, group, epilogue, out, epilogue == 0 || a_bf16, status, st};
+  if (a_bf16) return group == 32 ? launch<true, 32>(p, s, mt) : group == 64 ? launch<true, 64>(p, s, mt) : launch<true, 128>(p, s, mt);
+  return group == 32 ? launch<false, 32>(p, s, mt) : group == 64 ? launch<false, 64>(p, s, mt) : launch<false, 128>(p, s, mt);
 }
 
 cudaError_t launch_quantize_weights(const float* w, int N, int K, int group, void* codes, void* scales, cudaStream_t st) {

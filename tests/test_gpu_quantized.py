@@ -335,7 +335,7 @@ def unpack(w):
     for r in range(4):
         for e in range(2):
             codes[16 * tile + g + 8 * (r % 2), 64 * chunk + 32 * (s // 2) + 8 * t + 4 * (s % 2) + 2 * (r // 2) + e] = (words >> (4 * r + 16 * e) & 15) - 8
-    scales = w.scales.float().cpu().view(N // 16, K // w.group, 16).permute(0, 2, 1).reshape(N, -1)
+    scales = w.scales.float().cpu().view(N // 16, K // w.group, 8, 2).permute(0, 3, 2, 1).reshape(N, -1)
     return torch.from_numpy(codes).cuda(), scales.cuda()
 
 
@@ -399,6 +399,25 @@ def test_linear(models, operand, N, K, group, M):
             assert torch.equal(again, guard[:M])
 
 
+@pytest.mark.parametrize("operand", ["f16", "bf16"])
+@pytest.mark.parametrize("N,K,group", [(4752, 4160, 64), (4768, 4160, 32), (16384, 640, 128), (14240, 704, 32), (9600, 2112, 64)])
+@pytest.mark.parametrize("M", [1, 8, 13, 16, 20, 31, 41])
+def test_linear_of_large_matrices(models, operand, N, K, group, M):
+    """Matrices that flow through a ring: ragged last units, last stages and last groups of rows."""
+    m, gen = models[operand], gen_of(N + K + M)
+    q = m.quantize_weights(matrix(gen, N, K), group)
+    codes, scales = unpack(q)
+    a, bias, residual = randn(gen, M, K).to(TYPES[operand]), randn(gen, N), randn(gen, M, N)
+    out = residual.clone()
+    m.linear_quantized(a, q, bias, 1, out)
+    assert_linear(out, a, codes, scales, group, bias, 1, residual)
+    outs = [torch.empty(M, N, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for o in outs:
+        m.linear_quantized(a, q, bias, 0, o)
+    assert_linear(outs[0], a, codes, scales, group, bias, 0, None)
+    assert torch.equal(*outs)
+
+
 def test_every_code_and_a_scale_that_is_not_a_number(models):
     """-8, which the quantiser does not give, is a code like the others; a NaN scale reaches its outputs only."""
     for operand in TYPES:
@@ -412,7 +431,7 @@ def test_every_code_and_a_scale_that_is_not_a_number(models):
         torch.cuda.synchronize()
         m.linear_quantized(a, q, bias, 0, out)
         assert_linear(out, a, codes, scales, 64, bias, 0, None)
-        q.scales[5] = float("nan")                                   # tile 0, group 0, output 5
+        q.scales[10] = float("nan")                                  # tile 0, group 0, output 5
         torch.cuda.synchronize()
         m.linear_quantized(a, q, bias, 0, out)
         assert bool(out[:, 5].isnan().all()) and int(out.isnan().sum()) == 3

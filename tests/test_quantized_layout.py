@@ -69,3 +69,31 @@ def test_attention_cuts_fit_an_sm_and_cover_all_rows(lib):
                     tiles = (S + 63) // 64
                     mine = -(-(-(-tiles // s.cs)) // s.nk)
                     assert s.nst >= min(mine, 3 if s.nr > 1 else 2), at            # a stage is filled again one tile late
+
+
+class GemmShape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("stream", "warps", "nt", "wn", "cw", "nst")]
+
+
+def test_projection_cuts_fit_an_sm(lib):
+    pick, smem = lib._ZN6marche19gemm_quantized_pickEiiii, lib._ZN6marche19gemm_quantized_smemEiiRKNS_18QuantizedGemmShapeE
+    pick.restype, pick.argtypes = GemmShape, [C.c_int] * 4
+    smem.restype, smem.argtypes = C.c_size_t, [C.c_int, C.c_int, C.POINTER(GemmShape)]
+    seen = set()
+    for M in (1, 8, 9, 16, 17, 24, 25, 32, 33, 100, 65536):
+        for tiles in (1, 8, 48, 144, 148, 149, 256, 296, 300, 592, 600, 888, 1024, 1536, 4096):
+            for chunks in (1, 2, 3, 7, 8, 9, 12, 16, 17, 40, 64, 100, 127, 128, 129, 192, 1024):
+                for group in (32, 64, 128):
+                    if group == 128 and chunks % 2:
+                        continue
+                    s = pick(M, 16 * tiles, 64 * chunks, group)
+                    at = (M, tiles, chunks, group, [getattr(s, n) for n, _ in GemmShape._fields_])
+                    mt = min((M + 7) // 8, 4)
+                    if s.stream:
+                        assert (s.nt, mt, s.cw) in [(1, 1, 4), (1, 2, 2), (1, 3, 1), (2, 3, 1), (3, 3, 1), (1, 4, 1), (2, 4, 1), (3, 4, 1)], at
+                        assert 2 * s.wn <= (14 if s.nt <= 2 else 8) and s.nt * s.wn <= 32 and 3 <= s.nst <= 16, at
+                        assert smem(M, group, C.byref(s)) <= 220 * 1024, at
+                        seen.add((s.nt, mt))
+                    else:
+                        assert 1 <= s.warps <= 16 and smem(M, group, C.byref(s)) <= 48 * 1024, at
+    assert len(seen) >= 4
