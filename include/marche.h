@@ -480,7 +480,8 @@ int marche_gather_kv_quantized(marche_ctx* ctx, const marche_quantized_cache* ca
  *   kv_len  device int32 [batch] or NULL (all seq_len); clamped to 0 .. seq_len; nothing behind it is looked at.  A
  *           sample without keys gives zeros.
  *   o       A [batch*n][n_heads*head_dim] dense, 16-byte aligned
- * n_heads % n_kv_heads == 0 (MARCHE_EINVAL).  Relevance scores are not taken here: a block that yields them keeps a
+ * n_heads % n_kv_heads == 0 (MARCHE_EINVAL).  marche_tuning.attention_kernel forces the mma.sync or (both other
+ * values) the tcgen05 kernel, AUTO picks by rows, keys, head_dim and items.  Relevance scores are not taken here: a block that yields them keeps a
  * 16-bit cache.  Every shape is bit-reproducible. */
 int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, int n_heads,
                                const marche_quantized_cache* cache, const int32_t* kv_len, void* o, marche_stream stream);

@@ -932,9 +932,11 @@ int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, 
   if ((int64_t)n * (n_heads / kv.H) > (1 << 24) || (int64_t)kv.B * n * n_heads > INT32_MAX / 16) return MARCHE_ESHAPE;
   if (ld_q % 8 || (((uintptr_t)q | (uintptr_t)o) & 15)) return misaligned(ctx, "attention over an 8-bit cache");
   if (n == 0) return MARCHE_OK;
+  const int ak = ctx->tune.attention_kernel;
+  const bool tc = ak == MARCHE_ATTENTION_AUTO ? attention_quantized_tc_wins(n * (n_heads / kv.H), kv.S, kv.dh, kv.B * kv.H) : ak != MARCHE_ATTENTION_MMA;
   mark(ctx, MARCHE_KC_ATTENTION, (cudaStream_t)stream);
-  MARCHE_TRY(launch_attention_quantized(q, ld_q, n, n_heads, kv, kv_len, o, ctx->a_bf16, ctx->status_dev, (cudaStream_t)stream),
-             "attention_quantized");
+  MARCHE_TRY((tc ? launch_attention_quantized_tc : launch_attention_quantized)(q, ld_q, n, n_heads, kv, kv_len, o, ctx->a_bf16, ctx->status_dev,
+                                                                              (cudaStream_t)stream), "attention_quantized");
   return MARCHE_OK;
 }
 

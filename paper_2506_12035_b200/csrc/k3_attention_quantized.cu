@@ -2,19 +2,24 @@
 //
 // o = softmax(q K^T / sqrt(dh)) V with K[s] = ks[s] ck[s], V[s] = vs[s] cv[s], codes c in -127 .. 127 and one scale per key and head.
 // The scales are kept out of the products: the logit of a key is ks[s] (q . ck[s]), and vs[s] goes into the weight, so the tensor
-// cores multiply the codes themselves, which are exact in fp16.  q (bf16) is exact in fp16 after its row's power of two is taken off; what
+// cores multiply the codes themselves, which are exact in fp16.  q (bf16) is exact in fp16 after a power of two is taken off; what
 // is rounded is the weight: p vs / 2^e to fp16 (11 bits), where 2^e bounds the largest value scale met so far and the whole is
 // lifted by 2^14, so that a weight 2^-28 of the largest possible keeps all its bits.  Maxima, sums and accumulators are fp32, and the running
 // exponent e moves with the running maximum (one factor for both).
 // Query heads that share a cached head are rows of one item: row r is token r / G, head r % G of the group.
 //
-// mma.sync m16n8k16; codes become fp16 under the exponent of 1024 (a byte permute and a packed subtraction for two).  K: a dot product
-// does not mind the order of its terms, so a lane's 16 consecutive bytes of a key serve as its pairs of four k16 steps, no transposition and
-// one shared-memory load; V: ldmatrix.trans on pairs of bytes, whose even and odd bytes are two tiles of eight columns.
-// nr warps take 16 or 32 rows each; nk groups of them take the tiles of 64 keys (K, V and both scales, by TMA) in turn, each group with a
-// ring of nst stages that its first warp fills (a producer warp of its own would be the ninth: three warps on one quarter of the SM's
-// registers, 168 for each); a cluster of cs CTAs splits a long sequence.  (CTA, group) pairs merge in rank order in the CTA that owns
-// the row: bit-reproducible.  A sample without keys gives zeros.
+// mma.sync m16n8k16 on the transposed products, S^T = K q^T and O^T = V^T P^T: keys (then columns of V) are the 16-row operand and the
+// query rows come in eights, so one token costs half of what a 16-row tile of queries would, and the codes, converted once, serve all
+// NB eights of a warp.  K: a dot product does not mind the order of its terms, so a lane's 16 consecutive bytes of a key serve as its
+// operands of four k16 steps (bytes 0 and 2 of a word, then 1 and 3): no transposition and one shared-memory load; code + 128 as it
+// stands is a fp16 subnormal, (code + 128) 2^-24, which the tensor cores multiply exactly, and 128 times the sum of q is in the accumulator
+// beforehand.  V: ldmatrix.trans on pairs of bytes, whose even and odd bytes are rows g and g + 8 of the operand; here the sum over all keys would
+// leave too little of the result behind 128 times the weights' sum, so codes become numbers (1024 + code + 128, minus 1152).  P: the
+// accumulator's layout is turned by movmatrix.
+// nr warps take 8 NB rows each; nk groups of them take the tiles of 32 or 64 keys (K, V and both scales, by TMA) in turn, each group with a
+// ring of nst stages that its first warp fills (slot and phase are stepped: a division in that place cost more than the tile); a cluster of cs
+// CTAs splits a long sequence.  (CTA, group) pairs merge in rank order in the CTA that owns the row: bit-reproducible.  A sample without
+// keys gives zeros.
 #include <cuda.h>
 
 #include "attention_common.cuh"
@@ -30,12 +35,15 @@ namespace {
 using att::ex2_approx;
 using att::ldsm_x4_trans;
 
-constexpr int KT = 64;                     // keys per tile
 constexpr int kMaxStages = 16;             // of a CTA
 constexpr int kThreadsMax = 256;
 enum { ST_ATTENTION_QUANTIZED = 0x25 };
 
-template <int DH> struct Cfg {
+// Keys per tile: 64 where shared memory holds two tiles for each of eight warps.
+constexpr int tile_keys(int dh) { return dh == 128 ? 32 : 64; }
+
+template <int DH, int NB> struct Cfg {
+  static constexpr int KT = tile_keys(DH), NM = KT / 16;
   static constexpr int TILE = KT * DH;                     // K or V of a stage
   static constexpr int STAGE = 2 * TILE;
   static constexpr int SCALES = 2 * KT * 4;                // of a stage: K's, V's
@@ -50,33 +58,25 @@ template <int DH> MARCHE_DEVINL uint32_t piece(int r, int c) {
   if (DH == 128) return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4));
   return (uint32_t)(r * DH + (c << 4));
 }
-// First of the four values that lane t of a quad holds in k16 step s (two for the step's lower, two for its upper half).
+// First of the four values that lane t of a quad holds in k16 step s (the first and third for the step's lower, the others for its upper half).
 template <int DH> MARCHE_DEVINL int value_of(int s, int t) { return DH == 80 ? 16 * s + 4 * t : 16 * (4 * (s / 4) + t) + 4 * (s % 4); }
 
-MARCHE_DEVINL uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-MARCHE_DEVINL uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
-}
-MARCHE_DEVINL float2 lds_f2(uint32_t a) {
-  float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
-  return v;
-}
 MARCHE_DEVINL void ldsm_x2_trans(uint32_t addr, uint32_t& r0, uint32_t& r1) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(addr));
 }
 MARCHE_DEVINL void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two of the four signed bytes of a word (SEL picks them and puts 0x64 above each) as fp16: 1024 + (byte + 128) - 1152.
+// Bytes 0 and 2 (1 and 3) of a word of codes as fp16 subnormals, (code + 128) 2^-24.
+MARCHE_DEVINL uint32_t even_codes(uint32_t w) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(w), "r"(0x80808080u), "r"(0x00ff00ffu));   // (w ^ 80..) & 00ff..
+  return r;
+}
+MARCHE_DEVINL uint32_t odd_codes(uint32_t w) { return even_codes(w >> 8); }
+// Two of the four bytes of a word of codes + 128 (SEL picks them and puts 0x64 above each) as fp16: 1024 + (code + 128) - 1152.
 template <uint32_t SEL> MARCHE_DEVINL uint32_t two_of(uint32_t biased) {
   uint32_t r;
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(__byte_perm(biased, 0x64646464u, SEL)), "r"(0x64806480u));
@@ -87,22 +87,53 @@ MARCHE_DEVINL uint32_t pack_weights(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+MARCHE_DEVINL float2 unpack_f16x2(uint32_t u) {
+  __half2 h = *reinterpret_cast<__half2*>(&u);
+  return __half22float2(h);
+}
+// Packed fp32 pairs, one instruction for two values.
+MARCHE_DEVINL void mul2(float& a, float& b, float x, float y) {
+  const float2 r = __fmul2_rn(make_float2(a, b), make_float2(x, y));
+  a = r.x;
+  b = r.y;
+}
+MARCHE_DEVINL void add2(float& a, float& b, float x, float y) {
+  const float2 r = __fadd2_rn(make_float2(a, b), make_float2(x, y));
+  a = r.x;
+  b = r.y;
+}
+MARCHE_DEVINL void fma2(float& a, float& b, float m, float x, float y) {   // a m + x, b m + y
+  const float2 r = __ffma2_rn(make_float2(a, b), make_float2(m, m), make_float2(x, y));
+  a = r.x;
+  b = r.y;
+}
+MARCHE_DEVINL float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+MARCHE_DEVINL uint32_t turn8x8(uint32_t x) {               // an 8 x 8 matrix of 16-bit values, spread over the warp as fragments are
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
 MARCHE_DEVINL void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 MARCHE_DEVINL float pow2(int biased_exponent) { return __int_as_float(biased_exponent << 23); }
 
 // Grid: B * H * n_rb * cs CTAs, the cs of a cluster next to one another.
-template <int DH, int MT>
+template <int DH, int NB>
 __global__ void __launch_bounds__(kThreadsMax)
 attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16* __restrict__ q, int ld_q, int n, int heads, int H, int G, int B, int S,
                            int pad, const float* __restrict__ scales, const int32_t* __restrict__ kv_len, uint16_t* __restrict__ o, int o_bf16,
                            const QuantizedSplit sp, int* __restrict__ status) {
-  using C = Cfg<DH>;
-  constexpr int RPW = 16 * MT;                             // rows of a warp
+  using C = Cfg<DH, NB>;
+  constexpr int RPW = 8 * NB, KT = C::KT, NM = C::NM;      // rows of a warp
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t scale_base = base + (uint32_t)(sp.nk * sp.nst * C::STAGE), recv = scale_base + (uint32_t)(sp.nk * sp.nst * C::SCALES);
+  uint8_t* gen = smem_raw + (base - raw);
   const float* recv_gen = reinterpret_cast<const float*>(smem_raw + (recv - raw));
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages];   // full, empty
   __shared__ int abort_flags[2];
@@ -133,246 +164,268 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
   if (kv_len) len = min(max(kv_len[b], 0), S);
   const int tiles = (len + KT - 1) / KT;
   const int kt0 = (int)((long long)rank * tiles / sp.cs), n_tiles = (int)((long long)(rank + 1) * tiles / sp.cs) - kt0;
-  bool ok = true;
-  float m_run[MT][2], l_run[MT][2], c_row[MT][2], oacc[MT][C::CHUNKS][2][4];
-  int e_run = 14;                                          // biased exponent above every value scale so far (14: the lowest whose factors exist)
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    m_run[m][0] = m_run[m][1] = -INFINITY;
-    l_run[m][0] = l_run[m][1] = 0.f;
-#pragma unroll
-    for (int c = 0; c < C::CHUNKS; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) oacc[m][c][e >> 2][e & 3] = 0.f;
-  }
-  const bool active = row_w < R;
   const int mine = (n_tiles - wk + sp.nk - 1) / sp.nk, stage0 = wk * sp.nst;   // tiles wk, wk + nk, .. of the CTA's; the group's first stage
-  // Tile u of the group into its stage.
-  auto load = [&](int u) {
-    const int s = stage0 + u % sp.nst, kt = kt0 + wk + u * sp.nk;
+  // The group's next tile into its next stage (lane 0 of its first warp).
+  int f_slot = 0, issued = 0;
+  auto load = [&]() {
+    const int s = stage0 + f_slot, kt = kt0 + wk + issued * sp.nk;
     const uint32_t bar = full0 + 8u * s, dst = base + (uint32_t)(s * C::STAGE), dst_s = scale_base + (uint32_t)(s * C::SCALES);
     ptx::mbar_expect_tx(bar, C::STAGE + C::SCALES);
     ptx::tma_load_3d(dst, &tmap, h * DH, kt * KT, b, bar);
     ptx::tma_load_3d(dst + C::TILE, &tmap, h * DH, kt * KT, B + b, bar);
     bulk_load(dst_s, scales + ((size_t)b * H + h) * pad + (size_t)kt * KT, KT * 4, bar);
     bulk_load(dst_s + KT * 4, scales + ((size_t)(B + b) * H + h) * pad + (size_t)kt * KT, KT * 4, bar);
+    ++issued;
+    if (++f_slot == sp.nst) f_slot = 0;
   };
-  int issued = 0;                                          // by lane 0 of the group's first warp
   if (wr == 0 && lane == 0)
-    for (; issued < mine && issued < sp.nst; ++issued) load(issued);
+    while (issued < mine && issued < sp.nst) load();
   __syncwarp();
-  {
-    uint32_t qf[MT][C::STEPS][4];
-    if (active) {
-      const float scale_log2 = rsqrtf((float)DH) * 1.4426950408889634f;
+
+  // Rows 2 t and 2 t + 1 of each eight: running maximum (of the raw logits), this lane's part of the sum of weights; O^T: columns 16 c + 2 g (entries
+  // 0, 1 for the two rows) and 16 c + 2 g + 1 (2, 3).
+  bool ok = true;
+  const bool active = row_w < R;
+  float m_run[NB][2], l_run[NB][2], oacc[NB][C::CHUNKS][4];
+  int e_run = 14;                                          // biased exponent above every value scale so far (14: the lowest whose factors exist)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+  for (int m = 0; m < NB; ++m) {
+    m_run[m][0] = m_run[m][1] = -INFINITY;
+    l_run[m][0] = l_run[m][1] = 0.f;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int row = row_w + 16 * m + 8 * r + g, token = row / G;
-          const bf16* src = q + ((size_t)b * n + token) * ld_q + (h * G + row - token * G) * DH;
-          uint2 x[C::STEPS];
-          uint32_t top = 0;
+    for (int c = 0; c < C::CHUNKS; ++c) oacc[m][c][0] = oacc[m][c][1] = oacc[m][c][2] = oacc[m][c][3] = 0.f;
+  }
+  // ---- the warp's query rows as the operand of eight columns: lane (g, t) holds row g's values 0, 2 and 1, 3 of each step's four
+  uint32_t qf[NB][C::STEPS][2];
+  float c_log2 = 0.f, q_off[NB][2];
+  if (active) {
+    uint2 x[NB][C::STEPS];
+    uint32_t top = 0;
 #pragma unroll
-          for (int s = 0; s < C::STEPS; ++s) {
-            x[s] = row < R ? *reinterpret_cast<const uint2*>(src + value_of<DH>(s, t)) : make_uint2(0, 0);
-            top = max(max(top, max(x[s].x & 0x7fffu, (x[s].x >> 16) & 0x7fffu)), max(x[s].y & 0x7fffu, (x[s].y >> 16) & 0x7fffu));
-          }
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          // the row divided by its largest power of two: exact in fp16 (2^-24 of the largest value and less goes), and no overflow
-          const int e = min(max((int)(top >> 7), 1), 253);
-          const float f = pow2(254 - e);
-          c_row[m][r] = scale_log2 * pow2(e);
+    for (int m = 0; m < NB; ++m) {
+      const int row = min(row_w + 8 * m + g, R - 1), token = row / G;       // (rows behind the last are the last one again: not stored)
+      const bf16* src = q + ((size_t)b * n + token) * ld_q + (h * G + row - token * G) * DH;
 #pragma unroll
-          for (int s = 0; s < C::STEPS; ++s) {
-            const float2 lo = unpack_bf16x2(x[s].x), hi = unpack_bf16x2(x[s].y);
-            qf[m][s][r] = pack_weights(lo.x * f, lo.y * f);
-            qf[m][s][2 + r] = pack_weights(hi.x * f, hi.y * f);
-          }
-        }
+      for (int s = 0; s < C::STEPS; ++s) {
+        x[m][s] = *reinterpret_cast<const uint2*>(src + value_of<DH>(s, t));
+        const uint32_t big = max(max(x[m][s].x & 0x7fffu, (x[m][s].x >> 16) & 0x7fffu), max(x[m][s].y & 0x7fffu, (x[m][s].y >> 16) & 0x7fffu));
+        top = max(top, big < 0x7f80u ? big : 0u);          // (infinities and NaN stay what they are, in their row)
+      }
     }
-    int turn = 0, phase = 0;                               // stage of tile u in the group's ring, its fill's parity
-    for (int u = 0; u < mine; ++u) {
-      const int s = stage0 + turn;
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8u * s, (uint32_t)phase, abort_flag))) { ok = false; break; }
-      if (active) {
-        const uint32_t k_tile = base + (uint32_t)(s * C::STAGE), v_tile = k_tile + C::TILE;
-        const uint32_t ks = scale_base + (uint32_t)(s * C::SCALES), vs = ks + KT * 4;
-        const int left = len - (kt0 + wk + u * sp.nk) * KT;             // keys of this tile that count
-        float sacc[MT][8][4];
+    top = __reduce_max_sync(0xffffffffu, top);
+    // All rows divided by the largest value's power of two and lifted by 2^15, fp16's largest (a bf16 number below 2 stays below 65504): exact
+    // down to 2^-30 of the largest value, and no logit is off by more than 2^-40 of the largest ones'.
+    const int e = min(max((int)(top >> 7), 16), 254);
+    const float f = pow2(269 - e), scale_log2 = rsqrtf((float)DH) * 1.4426950408889634f;
+    c_log2 = scale_log2 * pow2(e);                          // (codes as subnormals: 2^24 over 2^15, the rest goes to the keys' scales)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t w[C::STEPS];
-          const int key = 8 * j + g;
-          if (DH == 80) {
+    for (int m = 0; m < NB; ++m) {
+      float sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < C::STEPS; ++k) w[k] = lds32(k_tile + (uint32_t)(key * DH + 16 * k + 4 * t));
-          } else {
+      for (int s = 0; s < C::STEPS; ++s) {
+        const float2 lo = unpack_bf16x2(x[m][s].x), hi = unpack_bf16x2(x[m][s].y);
+        qf[m][s][0] = pack_weights(lo.x * f, hi.x * f);
+        qf[m][s][1] = pack_weights(lo.y * f, hi.y * f);
+        const float2 u = unpack_f16x2(qf[m][s][0]), v = unpack_f16x2(qf[m][s][1]);
+        sum += (u.x + u.y) + (v.x + v.y);
+      }
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);         // of row g
+      sum *= -128.0f * 0x1p-24f;
+      q_off[m][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+      q_off[m][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+    }
+  }
+  int turn = 0, phase = 0, turn_before = 0, phase_before = 0;   // stage of tile u in the group's ring, its fill's parity; the tile's before it
+  for (int u = 0; u < mine; ++u) {
+    const int s = stage0 + turn;
+    if (!__all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8u * s, (uint32_t)phase, abort_flag))) { ok = false; break; }
+    if (active) {
+      const uint8_t* k_tile = gen + s * C::STAGE;
+      const uint32_t v_tile = base + (uint32_t)(s * C::STAGE + C::TILE);
+      float* ks = reinterpret_cast<float*>(gen + (scale_base - base) + s * C::SCALES);
+      float* vs = ks + KT;
+      const int left = len - (kt0 + wk + u * sp.nk) * KT;  // keys of this tile that count
+      if (left < KT) {                                     // scales behind the last key may be anything
+        for (int k = lane; k < KT; k += 32)
+          if (k >= left) ks[k] = vs[k] = 0.f;
+        __syncwarp();
+      }
+      // ---- S^T: lane (g, t) gets keys 16 i + g (entries 0, 1: rows 2 t, 2 t + 1) and 16 i + g + 8 (2, 3)
+      float sacc[NB][NM][4];
 #pragma unroll
-            for (int k = 0; k < C::STEPS / 4; ++k) {
-              const uint4 v = lds128(k_tile + piece<DH>(key, 4 * k + t));
-              w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
-            }
-          }
-#pragma unroll
-          for (int m = 0; m < MT; ++m) sacc[m][j][0] = sacc[m][j][1] = sacc[m][j][2] = sacc[m][j][3] = 0.f;
+      for (int i = 0; i < NM; ++i) {
+        uint32_t w0[C::STEPS], w1[C::STEPS];
+        const int key = 16 * i + g;
+        if (DH == 80) {
 #pragma unroll
           for (int k = 0; k < C::STEPS; ++k) {
-            const uint32_t u = w[k] ^ 0x80808080u, b0 = two_of<0x4140>(u), b1 = two_of<0x4342>(u);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) mma_f16(sacc[m][j], qf[m][k], b0, b1);
+            w0[k] = *reinterpret_cast<const uint32_t*>(k_tile + key * DH + 16 * k + 4 * t);
+            w1[k] = *reinterpret_cast<const uint32_t*>(k_tile + (key + 8) * DH + 16 * k + 4 * t);
           }
-          const float2 f = lds_f2(ks + (uint32_t)(8 * j + 2 * t) * 4u);
+        } else {
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            sacc[m][j][0] *= f.x; sacc[m][j][1] *= f.y;
-            sacc[m][j][2] *= f.x; sacc[m][j][3] *= f.y;
-          }
-        }
-        if (left < KT) {
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (8 * j + 2 * t + (e & 1) >= left) sacc[m][j][e] = -INFINITY;
-        }
-        // largest value scale of the tile (they are not negative: they order as integers; NaN counts as the largest number)
-        const float2 mine = lds_f2(vs + (uint32_t)lane * 8u);
-        uint32_t top = max(2 * lane < left ? __float_as_uint(mine.x) : 0u, 2 * lane + 1 < left ? __float_as_uint(mine.y) : 0u);
-        top = __reduce_max_sync(0xffffffffu, top);
-        const int e_new = max(e_run, min((int)(top >> 23), 254));
-        const float lift = pow2(267 - e_new);              // 2^14 over the power of two above the scale
-        float step = e_new == e_run ? 1.f : (e_new - e_run > 120 ? 0.f : pow2(127 - (e_new - e_run)));
-        e_run = e_new;
-        float neg[MT][2];
-        bool moved = step != 1.f;
-        float corr[MT][2];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fmaxf(sacc[m][j][2 * r], sacc[m][j][2 * r + 1]));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const float m_new = fmaxf(m_run[m][r], mx), ref = m_new == -INFINITY ? 0.f : m_new;
-            corr[m][r] = ex2_approx((m_run[m][r] - ref) * c_row[m][r]);
-            moved = moved || m_new != m_run[m][r];
-            m_run[m][r] = m_new;
-            neg[m][r] = -ref * c_row[m][r];
-          }
-        if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            l_run[m][0] *= corr[m][0];
-            l_run[m][1] *= corr[m][1];
-            const float c0 = corr[m][0] * step, c1 = corr[m][1] * step;
-#pragma unroll
-            for (int c = 0; c < C::CHUNKS; ++c)
-#pragma unroll
-              for (int p = 0; p < 2; ++p) {
-                oacc[m][c][p][0] *= c0; oacc[m][c][p][1] *= c0;
-                oacc[m][c][p][2] *= c1; oacc[m][c][p][3] *= c1;
-              }
+          for (int k = 0; k < C::STEPS / 4; ++k) {
+            const uint4 u0 = *reinterpret_cast<const uint4*>(k_tile + piece<DH>(key, 4 * k + t));
+            const uint4 u1 = *reinterpret_cast<const uint4*>(k_tile + piece<DH>(key + 8, 4 * k + t));
+            w0[4 * k] = u0.x; w0[4 * k + 1] = u0.y; w0[4 * k + 2] = u0.z; w0[4 * k + 3] = u0.w;
+            w1[4 * k] = u1.x; w1[4 * k + 1] = u1.y; w1[4 * k + 2] = u1.z; w1[4 * k + 3] = u1.w;
           }
         }
 #pragma unroll
-        for (int k2 = 0; k2 < KT / 16; ++k2) {
-          uint32_t pf[MT][4];
+        for (int m = 0; m < NB; ++m) {
+          sacc[m][i][0] = sacc[m][i][2] = q_off[m][0];
+          sacc[m][i][1] = sacc[m][i][3] = q_off[m][1];
+        }
+#pragma unroll
+        for (int k = 0; k < C::STEPS; ++k) {
+          const uint32_t a[4] = {even_codes(w0[k]), even_codes(w1[k]), odd_codes(w0[k]), odd_codes(w1[k])};
+#pragma unroll
+          for (int m = 0; m < NB; ++m) mma_f16(sacc[m][i], a, qf[m][k][0], qf[m][k][1]);
+        }
+        float f0 = ks[key], f1 = ks[key + 8];
+        f0 *= 512.0f;                                      // (2^24 over the rows' 2^15)
+        f1 *= 512.0f;
+#pragma unroll
+        for (int m = 0; m < NB; ++m) {
+          mul2(sacc[m][i][0], sacc[m][i][1], f0, f0);
+          mul2(sacc[m][i][2], sacc[m][i][3], f1, f1);
+        }
+      }
+      if (left < KT) {
+#pragma unroll
+        for (int m = 0; m < NB; ++m)
+#pragma unroll
+          for (int i = 0; i < NM; ++i) {
+            if (16 * i + g >= left) sacc[m][i][0] = sacc[m][i][1] = -INFINITY;
+            if (16 * i + g + 8 >= left) sacc[m][i][2] = sacc[m][i][3] = -INFINITY;
+          }
+      }
+      // ---- references: the largest value scale (they are not negative: they order as integers; NaN counts as the largest number), the rows' maxima
+      uint32_t top = __float_as_uint(vs[lane]);
+      if (KT == 64) top = max(top, __float_as_uint(vs[lane + KT / 2]));
+      top = __reduce_max_sync(0xffffffffu, top);
+      const int e_new = max(e_run, min((int)(top >> 23), 254));
+      const float lift = pow2(267 - e_new);                // 2^14 over the power of two above the scale
+      const float step = e_new == e_run ? 1.f : (e_new - e_run > 120 ? 0.f : pow2(127 - (e_new - e_run)));
+      e_run = e_new;
+      float neg[NB][2], corr[NB][2];
+      bool moved = step != 1.f;
+#pragma unroll
+      for (int m = 0; m < NB; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float mx = m_run[m][r];
+#pragma unroll
+          for (int i = 0; i < NM; ++i) mx = max3(mx, sacc[m][i][r], sacc[m][i][2 + r]);
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const float ref = mx == -INFINITY ? 0.f : mx;
+          corr[m][r] = ex2_approx((m_run[m][r] - ref) * c_log2);
+          moved = moved || mx != m_run[m][r];
+          m_run[m][r] = mx;
+          neg[m][r] = -ref * c_log2;
+        }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int m = 0; m < NB; ++m) {
+          mul2(l_run[m][0], l_run[m][1], corr[m][0], corr[m][1]);
+          mul2(corr[m][0], corr[m][1], step, step);
+#pragma unroll
+          for (int c = 0; c < C::CHUNKS; ++c) {
+            mul2(oacc[m][c][0], oacc[m][c][1], corr[m][0], corr[m][1]);
+            mul2(oacc[m][c][2], oacc[m][c][3], corr[m][0], corr[m][1]);
+          }
+        }
+      }
+      // ---- weights, turned, and O^T += V^T P^T
+      float ls[NB][2];
+#pragma unroll
+      for (int m = 0; m < NB; ++m) ls[m][0] = ls[m][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NM; ++i) {
+        uint32_t pb[NB][2];
+        float f0 = vs[16 * i + g], f1 = vs[16 * i + g + 8];
+        mul2(f0, f1, lift, lift);
+#pragma unroll
+        for (int m = 0; m < NB; ++m)
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            const int j = 2 * k2 + hf;
-            float2 f = lds_f2(vs + (uint32_t)(8 * j + 2 * t) * 4u);
-            f.x = 8 * j + 2 * t < left ? f.x * lift : 0.f;
-            f.y = 8 * j + 2 * t + 1 < left ? f.y * lift : 0.f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-              for (int r = 0; r < 2; ++r) {
-                const float p0 = ex2_approx(fmaf(sacc[m][j][2 * r], c_row[m][r], neg[m][r]));
-                const float p1 = ex2_approx(fmaf(sacc[m][j][2 * r + 1], c_row[m][r], neg[m][r]));
-                l_run[m][r] += p0 + p1;
-                pf[m][2 * hf + r] = pack_weights(p0 * f.x, p1 * f.y);
-              }
+            float p0 = sacc[m][i][2 * hf], p1 = sacc[m][i][2 * hf + 1];
+            fma2(p0, p1, c_log2, neg[m][0], neg[m][1]);
+            p0 = ex2_approx(p0);
+            p1 = ex2_approx(p1);
+            add2(ls[m][0], ls[m][1], p0, p1);
+            mul2(p0, p1, hf ? f1 : f0, hf ? f1 : f0);
+            pb[m][hf] = turn8x8(pack_weights(p0, p1));
           }
-          const int key = 16 * k2 + 8 * ((lane >> 3) & 1) + (lane & 7);
+        const int key = 16 * i + 8 * ((lane >> 3) & 1) + (lane & 7);
 #pragma unroll
-          for (int c = 0; c < C::CHUNKS; c += 2) {
-            uint32_t w[4];
-            if (c + 1 < C::CHUNKS) ldsm_x4_trans(v_tile + piece<DH>(key, c + (lane >> 4)), w[0], w[1], w[2], w[3]);
-            else ldsm_x2_trans(v_tile + piece<DH>(key, c), w[0], w[1]);
+        for (int c = 0; c < C::CHUNKS; c += 2) {
+          uint32_t w[4];
+          if (c + 1 < C::CHUNKS) ldsm_x4_trans(v_tile + piece<DH>(key, c + (lane >> 4)), w[0], w[1], w[2], w[3]);
+          else ldsm_x2_trans(v_tile + piece<DH>(key, c), w[0], w[1]);
 #pragma unroll
-            for (int d = 0; d < 2 && c + d < C::CHUNKS; ++d) {
-              const uint32_t lo = w[2 * d] ^ 0x80808080u, hi = w[2 * d + 1] ^ 0x80808080u;
-              const uint32_t e0 = two_of<0x4240>(lo), e1 = two_of<0x4240>(hi), o0 = two_of<0x4341>(lo), o1 = two_of<0x4341>(hi);
+          for (int d = 0; d < 2 && c + d < C::CHUNKS; ++d) {
+            const uint32_t lo = w[2 * d] ^ 0x80808080u, hi = w[2 * d + 1] ^ 0x80808080u;
+            const uint32_t a[4] = {two_of<0x4240>(lo), two_of<0x4341>(lo), two_of<0x4240>(hi), two_of<0x4341>(hi)};
 #pragma unroll
-              for (int m = 0; m < MT; ++m) {
-                mma_f16(oacc[m][c + d][0], pf[m], e0, e1);
-                mma_f16(oacc[m][c + d][1], pf[m], o0, o1);
-              }
-            }
+            for (int m = 0; m < NB; ++m) mma_f16(oacc[m][c + d], a, pb[m][0], pb[m][1]);
           }
         }
       }
-      __syncwarp();
-      if (lane == 0) {
-        ptx::mbar_arrive(empty0 + 8u * s);
-        // The stage of the tile before this one (of this one where no other warp reads it) is free, or nearly: its next tile.
-        const int from = sp.nr == 1 ? u : u - 1;
-        if (wr == 0 && from >= 0 && from + sp.nst < mine) {
-          const int f = stage0 + from % sp.nst;
-          if (ptx::mbar_wait(empty0 + 8u * f, (uint32_t)(from / sp.nst) & 1u, abort_flag)) { load(from + sp.nst); ++issued; }
-          else ok = false;
-        }
-      }
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-      if (!ok) break;
-      if (++turn == sp.nst) { turn = 0; phase ^= 1; }
-    }
-    if (!ok && wr == 0 && lane == 0) {                     // let copies already issued land before the CTA's shared memory is released
-      for (int u = issued > sp.nst ? issued - sp.nst : 0; u < issued; ++u)
-        ptx::mbar_wait(full0 + 8u * (stage0 + u % sp.nst), (uint32_t)(u / sp.nst) & 1u, abort_flag + 1, 20000000LL);
-    }
-    if (!ok && lane == 0) *(volatile int*)status = ST_ATTENTION_QUANTIZED;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 1);
-        l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 2);
-        if (!active) m_run[m][r] = -INFINITY;
+      for (int m = 0; m < NB; ++m) add2(l_run[m][0], l_run[m][1], ls[m][0], ls[m][1]);
+    }
+    __syncwarp();
+    if (lane == 0) {
+      ptx::mbar_arrive(empty0 + 8u * s);
+      // The stage of the tile before this one (of this one where no other warp reads it) is free, or nearly: its next tile.
+      if (wr == 0 && issued < mine && (sp.nr == 1 || u > 0)) {
+        const int f = stage0 + (sp.nr == 1 ? turn : turn_before);
+        if (ptx::mbar_wait(empty0 + 8u * f, (uint32_t)(sp.nr == 1 ? phase : phase_before), abort_flag)) load();
+        else ok = false;
       }
+    }
+    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    if (!ok) break;
+    turn_before = turn;
+    phase_before = phase;
+    if (++turn == sp.nst) { turn = 0; phase ^= 1; }
   }
+  if (!ok && wr == 0 && lane == 0) {                       // let copies already issued land before the CTA's shared memory is released
+    for (int u = issued > sp.nst ? issued - sp.nst : 0; u < issued; ++u)
+      ptx::mbar_wait(full0 + 8u * (stage0 + u % sp.nst), (uint32_t)(u / sp.nst) & 1u, abort_flag + 1, 20000000LL);
+  }
+  if (!ok && lane == 0) *(volatile int*)status = ST_ATTENTION_QUANTIZED;
+#pragma unroll
+  for (int m = 0; m < NB; ++m)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 4);
+      l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 8);
+      l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 16);
+    }
   const float unlift = pow2(e_run - 13);
   auto row_out = [&](int row) {                            // of the item's rows
     const int token = row / G;
     return o + (((size_t)b * n + token) * heads + h * G + row - token * G) * DH;
   };
   auto inverse = [](float l) { return l > 0.f ? 1.0f / l : l; };   // no key: zeros; NaN stays
-  auto store = [&](uint16_t* to, float4 v, float f) {
-    uint2 u;
-    u.x = pack_a16x2(v.x * f, v.y * f, o_bf16 != 0);
-    u.y = pack_a16x2(v.z * f, v.w * f, o_bf16 != 0);
-    *reinterpret_cast<uint2*>(to) = u;
-  };
   const int n_parts = sp.cs * sp.nk;
   if (n_parts == 1) {
     if (active && ok) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int m = 0; m < NB; ++m)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int row = row_w + 16 * m + 8 * r + g;
+          const int row = row_w + 8 * m + 2 * t + r;
           if (row < R) {
-            uint16_t* to = row_out(row) + 4 * t;
+            uint16_t* to = row_out(row) + 2 * g;
             const float f = inverse(l_run[m][r]) * unlift;
 #pragma unroll
-            for (int c = 0; c < C::CHUNKS; ++c)
-              store(to + 16 * c, make_float4(oacc[m][c][0][2 * r], oacc[m][c][1][2 * r], oacc[m][c][0][2 * r + 1], oacc[m][c][1][2 * r + 1]), f);
+            for (int c = 0; c < C::CHUNKS; ++c) *reinterpret_cast<uint32_t*>(to + 16 * c) = pack_a16x2(oacc[m][c][r] * f, oacc[m][c][2 + r] * f, o_bf16 != 0);
           }
         }
     }
@@ -387,19 +440,19 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
   }
   if (active && ok) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NB; ++m)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int in = wr * RPW + 16 * m + 8 * r + g, owner = in / own;
+        const int in = wr * RPW + 8 * m + 2 * t + r, owner = in / own;
         if (row_block + in < R) {
           uint32_t dst = recv + 4u * (uint32_t)(((rank * sp.nk + wk) * own + in - owner * own) * C::ROW);
           if (sp.cs > 1) dst = ptx::mapa(dst, (uint32_t)owner);
 #pragma unroll
           for (int c = 0; c < C::CHUNKS; ++c)
-            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 4u * (16 * c + 4 * t)), "f"(oacc[m][c][0][2 * r] * unlift),
-                         "f"(oacc[m][c][1][2 * r] * unlift), "f"(oacc[m][c][0][2 * r + 1] * unlift), "f"(oacc[m][c][1][2 * r + 1] * unlift) : "memory");
-          if (t == 0)                                      // the maximum in the exponent's own units
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * DH), "f"(m_run[m][r] * c_row[m][r]), "f"(l_run[m][r]) : "memory");
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * (16 * c + 2 * g)), "f"(oacc[m][c][r] * unlift),
+                         "f"(oacc[m][c][2 + r] * unlift) : "memory");
+          if (g == 0)                                      // the maximum in the exponent's own units
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * DH), "f"(m_run[m][r] * c_log2), "f"(l_run[m][r]) : "memory");
         }
       }
   }
@@ -426,70 +479,91 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
       acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y);
       acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
     }
-    store(row_out(row) + c, acc, inverse(l));
+    const float f = inverse(l);
+    uint2 v;
+    v.x = pack_a16x2(acc.x * f, acc.y * f, o_bf16 != 0);
+    v.y = pack_a16x2(acc.z * f, acc.w * f, o_bf16 != 0);
+    *reinterpret_cast<uint2*>(row_out(row) + c) = v;
   }
 }
 
-template <int DH, int MT>
-cudaError_t launch(const CUtensorMap& tm, const void* q, int ld_q, int n, int heads, const QuantizedKv& c, const int32_t* kv_len, void* o, bool o_bf16,
-                   const QuantizedSplit& s, int* status, cudaStream_t st) {
+template <int DH, int NB>
+cudaError_t launch(const void* q, int ld_q, int n, int heads, const QuantizedKv& c, const int32_t* kv_len, void* o, bool o_bf16, const QuantizedSplit& s,
+                   int* status, cudaStream_t st) {
+  using C = Cfg<DH, NB>;
   const size_t smem = attention_quantized_smem(DH, s);
   if (smem > 226 * 1024) return cudaErrorInvalidValue;
+  CUtensorMap tm;
+  EncodeTiledFn fn = tma_encode_fn();
+  const cuuint64_t D = (cuuint64_t)c.H * DH, dims[3] = {D, (cuuint64_t)c.S, (cuuint64_t)2 * c.B}, strides[2] = {D, D * c.S};
+  const cuuint32_t box[3] = {DH, C::KT, 1}, unit[3] = {1, 1, 1};
+  const CUtensorMapSwizzle sw = DH == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : DH == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
+  if (!fn || fn(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, c.codes, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
-  cudaError_t e = ensure_dynamic_smem(attention_quantized_kernel<DH, MT>, smem, smem_set);
+  cudaError_t e = ensure_dynamic_smem(attention_quantized_kernel<DH, NB>, smem, smem_set);
   if (e != cudaSuccess) return e;
   const int G = heads / c.H;
-  return launch_pdl_cluster(attention_quantized_kernel<DH, MT>, dim3((unsigned)((long)c.B * c.H * s.n_rb * s.cs)), dim3(s.nr * s.nk * 32), smem, s.cs, st, tm,
+  return launch_pdl_cluster(attention_quantized_kernel<DH, NB>, dim3((unsigned)((long)c.B * c.H * s.n_rb * s.cs)), dim3(s.nr * s.nk * 32), smem, s.cs, st, tm,
                             (const bf16*)q, ld_q, n, heads, c.H, G, c.B, c.S, c.pad, (const float*)c.scales, kv_len, (uint16_t*)o, o_bf16 ? 1 : 0, s, status);
 }
 
 }  // namespace
 
+// Which kernel: by estimated time (us).  This one: a warp of 16 rows takes a tile of 64 keys in 0.3 us of an SM's time where the SMs are full (0.4 where
+// a warp or two are on each), and splits long sequences; the tcgen05 one 0.8 us for 128 rows, but not less than 1.3 us a tile in turn.  Measured, this
+// one and tcgen05, us: head_dim 64, 2048 items, S 320: 43 rows 61 and 67, 64 rows 75 and 68, 128 rows 152 and 83; 512 items, S 1088: 32 rows 46
+// and 47, 43 rows 53 and 49, 200 rows 189 and 104; 128 items 43 rows 22.2 and 24.6, 64 rows 27.7 and 24.2; 32 items 128 rows 21.5 and 23.6;
+// 24 items, S 5000, 200 rows 57 and 87; head_dim 80, 2048 items, S 320, 43 rows 68 and 75; head_dim 128, 512 items, S 1088, 32 rows 74 and 98, 64
+// rows 126 and 101.
+bool attention_quantized_tc_wins(int R, int S, int dh, int items) {
+  if (R <= 16) return false;
+  const double sms = device_sm_count(), tiles = (S + 63) / 64, warp_tiles = (double)items * ((R + 15) / 16) * tiles / sms, units = (double)items * ((R + 127) / 128);
+  const double mma = 5.0 + warp_tiles * ((dh == 64 ? 0.3 : (dh == 80 ? 0.325 : 0.65)) + (warp_tiles < 100 ? 0.1 : 0.0));
+  const double a_tile = dh == 64 ? 0.8 : (dh == 80 ? 0.88 : 1.55), a_unit = dh == 128 ? 3.5 : 0.7, busy = units / sms * (tiles * a_tile + a_unit);
+  return 4.0 + (busy > tiles * 1.3 ? busy : tiles * 1.3) < mma;
+}
+
 QuantizedSplit attention_quantized_plan(int R, int S, int dh, int items) {
-  const int tiles = (S + KT - 1) / KT, sms = device_sm_count();
+  const int sms = device_sm_count(), eights = (R + 7) / 8;
   QuantizedSplit s;
-  s.mt = R > 16 && dh != 128 ? 2 : 1;
-  const int rpw = 16 * s.mt, groups = (R + rpw - 1) / rpw;
-  s.n_rb = (groups + 3) / 4;
-  s.nr = (groups + s.n_rb - 1) / s.n_rb;
+  const int warps = (eights + 1) / 2;                      // along the rows
+  s.nb = (eights + warps - 1) / warps;
+  s.n_rb = (warps + 2) / 3;
+  s.nr = (warps + s.n_rb - 1) / s.n_rb;
+  const int kt = tile_keys(dh), tiles = (S + kt - 1) / kt;
   const long blocks = (long)items * s.n_rb;
   s.cs = 1;
   while (s.cs < 8 && blocks * s.cs < 2 * sms && tiles > 4 * s.cs) s.cs *= 2;
   const int per = (tiles + s.cs - 1) / s.cs;
   // (a stage is filled again one tile late where other warps read it, too: three of them)
-  const int stage = 2 * KT * dh + 2 * KT * 4, least = s.nr > 1 ? 3 : 2;
-  s.nk = 1;
-  while (2 * s.nk * s.nr <= 8 && 2 * s.nk <= per && 2 * s.nk * least * stage <= 150 * 1024 && blocks * s.cs * s.nk < 6 * sms) s.nk *= 2;
-  const int mine = (per + s.nk - 1) / s.nk, most = kMaxStages / s.nk;
+  const int stage = 2 * kt * dh + 2 * kt * 4, least = s.nr > 1 ? 3 : 2;
+  const long want = (6L * sms + blocks * s.cs - 1) / (blocks * s.cs);   // six groups on an SM, if the tiles go round
+  s.nk = 8 / s.nr < per ? 8 / s.nr : per;
+  if (s.nk > want) s.nk = (int)want;
+  while (s.nk > 1 && s.nk * least * stage > 150 * 1024) --s.nk;
+  const int mine = (per + s.nk - 1) / s.nk, fit = kMaxStages / s.nk;
   s.nst = mine < least ? mine : least;
-  while (s.nst < mine && s.nst < most && s.nk * (s.nst + 1) * stage <= 40 * 1024) ++s.nst;
+  while (s.nst < mine && s.nst < fit && s.nk * (s.nst + 1) * stage <= 40 * 1024) ++s.nst;
   return s;
 }
 
 // Shared memory of a CTA: the rings, and the partial results where there are several of a row.
 size_t attention_quantized_smem(int dh, const QuantizedSplit& s) {
-  const int parts = s.cs * s.nk, own = (s.nr * 16 * s.mt + s.cs - 1) / s.cs;
-  return 1024 + (size_t)s.nk * s.nst * (2 * KT * dh + 2 * KT * 4) + (parts > 1 ? (size_t)parts * own * (dh + 4) * 4 : 0);
+  const int parts = s.cs * s.nk, own = (s.nr * 8 * s.nb + s.cs - 1) / s.cs, kt = tile_keys(dh);
+  return 1024 + (size_t)s.nk * s.nst * (2 * kt * dh + 2 * kt * 4) + (parts > 1 ? (size_t)parts * own * (dh + 4) * 4 : 0);
 }
 
 cudaError_t launch_attention_quantized(const void* q, int ld_q, int n, int heads, const QuantizedKv& c, const int32_t* kv_len, void* o, bool o_bf16,
                                        int* status, cudaStream_t st) {
-  CUtensorMap tm;
-  EncodeTiledFn fn = tma_encode_fn();
-  const cuuint64_t D = (cuuint64_t)c.H * c.dh, dims[3] = {D, (cuuint64_t)c.S, (cuuint64_t)2 * c.B}, strides[2] = {D, D * c.S};
-  const cuuint32_t box[3] = {(cuuint32_t)c.dh, KT, 1}, unit[3] = {1, 1, 1};
-  const CUtensorMapSwizzle sw = c.dh == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : c.dh == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
-  if (!fn || fn(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, c.codes, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return cudaErrorInvalidValue;
   const QuantizedSplit s = attention_quantized_plan(n * (heads / c.H), c.S, c.dh, c.B * c.H);
-  switch (c.dh) {
-    case 64:
-      return s.mt == 2 ? launch<64, 2>(tm, q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st) : launch<64, 1>(tm, q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st);
-    case 80:
-      return s.mt == 2 ? launch<80, 2>(tm, q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st) : launch<80, 1>(tm, q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st);
-    case 128: return launch<128, 1>(tm, q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st);
+#define MARCHE_QA(DH_, NB_) \
+  case DH_ * 8 + NB_: return launch<DH_, NB_>(q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st);
+  switch (c.dh * 8 + s.nb) {
+    MARCHE_QA(64, 1) MARCHE_QA(64, 2) MARCHE_QA(80, 1) MARCHE_QA(80, 2) MARCHE_QA(128, 1) MARCHE_QA(128, 2)
   }
+#undef MARCHE_QA
   return cudaErrorInvalidValue;
 }
 

@@ -171,13 +171,18 @@ cudaError_t launch_scatter_kv_quantized(const void* k, const void* v, int ld, co
 cudaError_t launch_gather_kv_quantized(const QuantizedKv& cache, const int32_t* idx, int n, void* k_out, void* v_out, int ld, cudaStream_t st);
 
 // K3 over such a cache: n query rows per sample, heads % cache.H == 0; kv_len [B] or NULL.  ld_q % 8 == 0, q 16-byte, o 8-byte aligned.
-// How a launch is cut: nr warps of 16 mt rows by nk groups along the key tiles in a CTA, nst stages for each group, n_rb blocks of rows, cs CTAs
+// How a launch is cut: nr warps of 8 nb rows by nk groups along the key tiles in a CTA, nst stages for each group, n_rb blocks of rows, cs CTAs
 // along the keys.  R rows of an item (query rows that share a cached head).
-struct QuantizedSplit { int mt, nr, nk, nst, cs, n_rb; };
+struct QuantizedSplit { int nb, nr, nk, nst, cs, n_rb; };
 QuantizedSplit attention_quantized_plan(int R, int S, int dh, int items);
 size_t attention_quantized_smem(int dh, const QuantizedSplit& s);
 cudaError_t launch_attention_quantized(const void* q, int ld_q, int n, int heads, const QuantizedKv& cache, const int32_t* kv_len, void* o,
                                        bool o_bf16, int* status, cudaStream_t st);
+
+// The same on tcgen05, for many rows (R of an item).
+bool attention_quantized_tc_wins(int R, int S, int dh, int items);
+cudaError_t launch_attention_quantized_tc(const void* q, int ld_q, int n, int heads, const QuantizedKv& cache, const int32_t* kv_len, void* o,
+                                          bool o_bf16, int* status, cudaStream_t st);
 
 // K2 on weights of 4 bits.  N % 16 == 0, K % 64 == 0, group 32, 64 or 128 dividing K; lda % 8 == 0, 16-byte aligned operands.
 struct QuantizedGemmShape { int stream, warps, nt, wn, cw, nst; };

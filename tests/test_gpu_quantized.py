@@ -4,7 +4,12 @@ Tolerances are bounds, from the roundings that the kernels make:
   codes, scales, values read back   none: equal bit by bit to the definition
   attention   o is a mean of values v with weights p; what is rounded is p vs (fp16: half a step is 2^-11 of it) and the result
               (half a step of its type), so |err| <= 2^-11 A + half |o| with A = sum p |v| / sum p; logits, exponentials and sums in fp32
-              add less than 2^-13 A at these sizes (logits of |x| < 2^5: 2^-18 of p at most by x's own rounding and the products' sums)
+              add less than 2^-13 A at these sizes (logits of |x| < 2^5: 2^-18 of p at most by x's own rounding and the products' sums).
+              fp16 ends: a weight far below the largest is a subnormal, off by up to 2^-25 of its unit, which is 2^-7 of a power of two
+              2^e that is at most twice the largest value scale, vmax / 127, of the (sample, head).  A key's term p v is then off by
+              2^-25 2^-7 (2 vmax / 127) 127 = 2^-31 vmax, S keys' by S 2^-31 vmax, and the sum of weights that all is divided by is
+              at least 1, the weight of the key that the reference is.  (It shows where A is nothing beside vmax: a column in which
+              the one key that counts holds a zero.)
   linear      products are exact; sums of a group (8 steps of the tensor core, 2^-23 each, which may truncate) and of groups and
               warps (2^-24 each) are relative to sum |a w|; then half a step of the output's type; GELU's slope is below 1.13
 """
@@ -157,11 +162,11 @@ def test_prefix_written_without_index(models):
 
 # ------------------------------------------------------------------ attention
 def reference(cache, q, n, heads, kv_len):
-    """o and the mean magnitude A, float64 [B*n][heads][dh]."""
+    """o, the mean magnitude A and S 2^-31 vmax, float64 [B*n][heads][dh]."""
     B, S, Hkv, dh = cache.B, cache.S, cache.n_kv_heads, cache.head_dim
     kv = values(cache)
     q = q.double().reshape(B, n, heads, dh)
-    o, A = torch.zeros_like(q), torch.zeros_like(q)
+    o, A, low = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(q)
     for b in range(B):
         length = S if kv_len is None else min(max(int(kv_len[b]), 0), S)
         if length == 0:
@@ -169,8 +174,21 @@ def reference(cache, q, n, heads, kv_len):
         for h in range(heads):
             k, v = kv[0, b, :length, h * Hkv // heads], kv[1, b, :length, h * Hkv // heads]
             p = torch.softmax(q[b, :, h] @ k.t() / dh ** 0.5, -1)
-            o[b, :, h], A[b, :, h] = p @ v, p @ v.abs()
-    return o.view(B * n, heads, dh), A.view(B * n, heads, dh)
+            o[b, :, h], A[b, :, h], low[b, :, h] = p @ v, p @ v.abs(), length * 2.0 ** -31 * v.abs().max()
+    return o.view(B * n, heads, dh), A.view(B * n, heads, dh), low.view(B * n, heads, dh)
+
+
+KERNELS = {"auto": binding.ATTENTION_AUTO, "mma": binding.ATTENTION_MMA, "tcgen05": binding.ATTENTION_TCGEN05}
+
+
+@pytest.fixture(params=["mma", "tcgen05"])
+def both_kernels(request, models):
+    """Each attention kernel asked for by name."""
+    for m in models.values():
+        m.set_tuning(attention_kernel=KERNELS[request.param])
+    yield request.param
+    for m in models.values():
+        m.set_tuning(attention_kernel=binding.ATTENTION_AUTO)
 
 
 def attend(m, cache, q, ld, n, heads, kv_len, o=None):
@@ -180,9 +198,9 @@ def attend(m, cache, q, ld, n, heads, kv_len, o=None):
 
 
 def assert_attention(o, cache, q, n, heads, kv_len):
-    want, A = reference(cache, q, n, heads, kv_len)
+    want, A, low = reference(cache, q, n, heads, kv_len)
     err = (o.double().view_as(want) - want).abs()
-    limit = (2.0 ** -11 + 2.0 ** -13) * A + HALF[o.dtype] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -24   # (fp16's smallest steps)
+    limit = (2.0 ** -11 + 2.0 ** -13) * A + low + HALF[o.dtype] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -24   # (fp16's smallest steps)
     worst = (err / limit.clamp_min(1e-30)).max()
     assert bool((err <= limit).all()), "error %.3g of the bound" % float(worst)
 
@@ -196,7 +214,7 @@ SHAPES = [  # B, S, heads, cached heads, rows
 @pytest.mark.parametrize("dh", [64, 80, 128])
 @pytest.mark.parametrize("operand", ["f16", "bf16"])
 @pytest.mark.parametrize("B,S,heads,kv_heads,n", SHAPES)
-def test_attention(models, dh, operand, B, S, heads, kv_heads, n):
+def test_attention(models, both_kernels, dh, operand, B, S, heads, kv_heads, n):
     m, gen = models[operand], gen_of(S + n + dh)
     cache = filled_cache(m, gen, B, S, kv_heads, dh)
     ld = heads * dh + 24
@@ -207,9 +225,27 @@ def test_attention(models, dh, operand, B, S, heads, kv_heads, n):
     assert torch.equal(o, attend(m, cache, q, ld, n, heads, None))    # bit-reproducible
 
 
+@pytest.mark.parametrize("dh", [64, 80, 128])
+@pytest.mark.parametrize("B,S,heads,kv_heads,n", [(150, 70, 2, 2, 50), (1, 130, 300, 150, 70), (7, 200, 16, 16, 300), (300, 320, 2, 2, 20)])
+def test_attention_of_many_items(models, both_kernels, dh, B, S, heads, kv_heads, n):
+    """More units than SMs and streams: several turns, full and short last tiles, samples of all lengths among them."""
+    m, gen = models["f16"], gen_of(B + S + dh)
+    cache = filled_cache(m, gen, B, S, kv_heads, dh)
+    kv_len = torch.randint(-1, S + 2, (B,), generator=gen, device="cuda", dtype=torch.int32)
+    q = randn(gen, B * n, heads * dh).to(torch.bfloat16)
+    for lens in (None, kv_len):
+        o = attend(m, cache, q, heads * dh, n, heads, lens)
+        some = torch.randperm(B, generator=gen, device="cuda")[:4].tolist()
+        for b in some:
+            part = QuantizedCache(cache.codes[:, b:b + 1].contiguous(), cache.scales[:, b:b + 1].contiguous(), kv_heads)
+            rows = slice(b * n, (b + 1) * n)
+            assert_attention(o[rows], part, q[rows], n, heads, None if lens is None else lens[b:b + 1])
+        assert torch.equal(o, attend(m, cache, q, heads * dh, n, heads, lens))
+
+
 @pytest.mark.parametrize("dh,n,heads", [(64, 1, 4), (80, 40, 4), (128, 3, 8), (64, 150, 4)])
 @pytest.mark.parametrize("lens", [[0, 1, 63, 64, 65, 700], [700, -5, 9999, 2, 0, 640], [0, 0, 0, 0, 0, 0]])
-def test_samples_of_different_lengths(models, dh, n, heads, lens):
+def test_samples_of_different_lengths(models, both_kernels, dh, n, heads, lens):
     """Keys behind a sample's length are not looked at (their scales are NaN here); none at all: zeros."""
     m, gen, B, S, kv = models["bf16"], gen_of(n), 6, 700, 4
     cache = filled_cache(m, gen, B, S, kv, dh)
@@ -227,7 +263,7 @@ def test_samples_of_different_lengths(models, dh, n, heads, lens):
 
 @pytest.mark.parametrize("dh", [64, 80, 128])
 @pytest.mark.parametrize("n", [1, 20, 140])
-def test_peaked_rows_and_scales_far_apart(models, dh, n):
+def test_peaked_rows_and_scales_far_apart(models, both_kernels, dh, n):
     """Logits of tens, and keys whose value scales lie up to 2^40 apart, in both orders: the weight that counts keeps its bits."""
     m, gen, B, S, H = models["f16"], gen_of(n + dh), 2, 400, 2
     cache = filled_cache(m, gen, B, S, H, dh, spread=False)
@@ -236,13 +272,13 @@ def test_peaked_rows_and_scales_far_apart(models, dh, n):
     cache.scales[1, 1, :, :S] *= torch.exp2(torch.linspace(10, -30, S, device="cuda"))
     q = (2.0 * randn(gen, B * n, H * dh)).to(torch.bfloat16)
     o = attend(m, cache, q, H * dh, n, H, None)
-    want, A = reference(cache, q, n, H, None)
+    want, A, low = reference(cache, q, n, H, None)
     # sums of |q k| reach 2^9 here: the fp32 logits are off by up to 2^9 2^-20, and every weight by twice that share
-    limit = (2.0 ** -11 + 2.0 ** -9.5) * A + HALF[o.dtype] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -24
+    limit = (2.0 ** -11 + 2.0 ** -9.5) * A + low + HALF[o.dtype] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -24
     assert bool(((o.double().view_as(want) - want).abs() <= limit).all())
 
 
-def test_query_rows_of_any_size(models):
+def test_query_rows_of_any_size(models, both_kernels):
     """A row of zeros weighs all keys alike; rows near the ends of bf16's range stay finite where the result is."""
     m, gen, B, S, H, dh, n = models["bf16"], gen_of(3), 1, 100, 1, 64, 20
     cache = filled_cache(m, gen, B, S, H, dh)
@@ -259,7 +295,7 @@ def test_query_rows_of_any_size(models):
     assert_attention(o[3:], cache, q[3:], n - 3, H, None)
 
 
-def test_a_key_that_is_not_a_number_reaches_its_sample_and_head_only(models):
+def test_a_key_that_is_not_a_number_reaches_its_sample_and_head_only(models, both_kernels):
     m, gen, B, S, H, dh, n = models["f16"], gen_of(4), 2, 130, 2, 64, 5
     cache = filled_cache(m, gen, B, S, H, dh)
     cache.scales[0, 1, 0, 129] = float("nan")
@@ -268,7 +304,7 @@ def test_a_key_that_is_not_a_number_reaches_its_sample_and_head_only(models):
     assert bool(bad[1, :, 0].all()) and int(bad.sum()) == n * dh
 
 
-def test_a_cache_beyond_32_bit_offsets(models):
+def test_a_cache_beyond_32_bit_offsets(models, both_kernels):
     """2^31 codes lie in front of V's last rows: written, read back and attended there."""
     m, gen, B, S, H, dh, n = models["bf16"], gen_of(5), 1, (1 << 20) + 77, 16, 80, 4
     cache = m.alloc_quantized_cache(B, S, H, dh)
@@ -294,7 +330,7 @@ def test_a_cache_beyond_32_bit_offsets(models):
     assert bool(((o - want).abs() <= limit).all())
 
 
-def test_attention_on_a_stream_and_in_a_graph(models):
+def test_attention_on_a_stream_and_in_a_graph(models, both_kernels):
     """Two captured calls that share nothing but the context, replayed with new inputs in the same buffers."""
     m, gen, B, S, H, dh = models["f16"], gen_of(6), 2, 1500, 4, 64
     cache = filled_cache(m, gen, B, S, H, dh)

@@ -48,7 +48,7 @@ def test_null_arguments(lib):
 
 
 class Split(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("mt", "nr", "nk", "nst", "cs", "n_rb")]
+    _fields_ = [(n, C.c_int) for n in ("nb", "nr", "nk", "nst", "cs", "n_rb")]
 
 
 def test_attention_cuts_fit_an_sm_and_cover_all_rows(lib):
@@ -63,10 +63,10 @@ def test_attention_cuts_fit_an_sm_and_cover_all_rows(lib):
                 for items in (1, 2, 8, 12, 24, 32, 60, 74, 75, 148, 149, 300, 592, 900, 2048):
                     s = plan(R, S, dh, items)
                     at = (dh, R, S, items, [getattr(s, n) for n, _ in Split._fields_])
-                    assert s.mt in (1, 2) and s.nr >= 1 and s.nk >= 1 and s.nst >= 1 and s.cs in (1, 2, 4, 8), at
+                    assert s.nb in (1, 2) and s.nr >= 1 and s.nk >= 1 and s.nst >= 1 and s.cs in (1, 2, 4, 8), at
                     assert s.nr * s.nk <= 8 and s.nk * s.nst <= 16 and smem(dh, C.byref(s)) <= 226 * 1024, at
-                    assert s.n_rb * s.nr * 16 * s.mt >= R and (s.n_rb - 1) * s.nr * 16 * s.mt < R, at
-                    tiles = (S + 63) // 64
+                    assert s.n_rb * s.nr * 8 * s.nb >= R and (s.n_rb - 1) * s.nr * 8 * s.nb < R, at
+                    tiles = -(-S // (32 if dh == 128 else 64))
                     mine = -(-(-(-tiles // s.cs)) // s.nk)
                     assert s.nst >= min(mine, 3 if s.nr > 1 else 2), at            # a stage is filled again one tile late
 
@@ -97,3 +97,13 @@ def test_projection_cuts_fit_an_sm(lib):
                     else:
                         assert 1 <= s.warps <= 16 and smem(M, group, C.byref(s)) <= 48 * 1024, at
     assert len(seen) >= 4
+
+
+@pytest.mark.parametrize("R,S,dh,items,want", [
+    (1, 1 << 20, 64, 4096, False), (16, 320, 64, 2048, False), (43, 320, 64, 2048, False), (64, 320, 64, 2048, True), (43, 1088, 64, 512, True),
+    (43, 1088, 64, 128, False), (64, 1088, 64, 128, True), (128, 1088, 64, 32, False), (200, 5000, 64, 24, False), (43, 320, 80, 2048, False),
+    (1088, 1088, 64, 512, True), (32, 1088, 128, 512, False), (64, 1088, 128, 512, True)])
+def test_which_attention(lib, R, S, dh, items, want):
+    wins = lib._ZN6marche27attention_quantized_tc_winsEiiii
+    wins.restype = C.c_bool
+    assert wins(R, S, dh, items) is want
