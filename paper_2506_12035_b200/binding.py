@@ -208,20 +208,24 @@ class QuantizedCache:
         assert tuple(scales.shape) == (2, B, n_kv_heads, (S + 63) // 64 * 64), "scales [2][B][kv_heads][S rounded up to 64]"
         self.codes, self.scales = codes, scales
         self.B, self.S, self.n_kv_heads, self.head_dim = B, S, n_kv_heads, D // n_kv_heads
+        self.width, self.device_index = D, codes.get_device()
         self.c = MarcheQuantizedCache(codes.data_ptr(), scales.data_ptr(), B, S, n_kv_heads, self.head_dim)
         self.ref = C.addressof(self.c)
 
     def check_rows(self, t: torch.Tensor, ld: int, n: int, width: int = 0):
-        """B * n rows of `width` (the cache's by default) bf16 values, `ld` values apart, lie in t's storage."""
-        rows = self.B * n
-        assert t.dtype == torch.bfloat16 and t.device == self.codes.device, "bf16 rows on the cache's device"
+        """B * n rows of `width` (the cache's by default) bf16 values, `ld` values apart, lie in t or, from its start on, in its storage."""
+        width, rows = width or self.width, self.B * n
+        assert t.dtype is torch.bfloat16 and t.get_device() == self.device_index, "bf16 rows on the cache's device"
+        if t.dim() == 2 and t.stride() == (ld, 1) and t.shape[0] >= rows and t.shape[1] >= width:
+            return
         if rows > 0:
-            need = t.storage_offset() + (rows - 1) * ld + (width or self.codes.shape[3])
+            need = t.storage_offset() + (rows - 1) * ld + width
             assert 2 * need <= t.untyped_storage().nbytes(), "fewer rows than the call names"
 
     def index(self, t: Optional[torch.Tensor], n: int) -> Optional[int]:
-        if t is not None:
-            assert t.dtype == torch.int32 and t.numel() >= self.B * n, "int32, one entry for every row"
+        if t is None:
+            return None
+        assert t.dtype is torch.int32 and t.numel() >= self.B * n, "int32, one entry for every row"
         return _ptr(t)
 
 

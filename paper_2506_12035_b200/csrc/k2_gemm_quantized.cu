@@ -192,17 +192,16 @@ gemm_quantized_small_kernel(const uint16_t* __restrict__ a, int lda, int M, cons
 }
 
 constexpr int kMaxStages = 16;
-constexpr int WK = 2;                      // warps that share tiles and split K
 enum { ST_GEMM_QUANTIZED = 0x66 };
 
-// Of a stage: 2 CW chunks of the rows (a chunk's 128 bytes under TMA's 128-byte swizzle, eight rows 1 KB), of the unit's tiles, and their scales.
-template <int MT, int CW, int G> struct Stage {
+// Of a stage: WK CW chunks of the rows (a chunk's 128 bytes under TMA's 128-byte swizzle, eight rows 1 KB), of the unit's tiles, and their scales.
+template <int MT, int WK, int CW, int G> struct Stage {
   static constexpr int CHUNKS = WK * CW, GROUPS = CHUNKS * kChunk / G, ROWS = CHUNKS * MT * 1024, CODES = CHUNKS * 512, SCALES = GROUPS * 32;
   static_assert(CHUNKS * kChunk % G == 0, "whole groups");
 };
-inline size_t stage_bytes_of(int mt, int cw, int group, int tiles) {
-  const size_t codes = (size_t)tiles * WK * cw * 512, scales = (size_t)tiles * (WK * cw * kChunk / group) * 32;
-  return ((size_t)WK * cw * mt * 1024 + codes + scales + 1023) / 1024 * 1024;
+inline size_t stage_bytes_of(int mt, int chunks, int group, int tiles) {
+  const size_t codes = (size_t)tiles * chunks * 512, scales = (size_t)tiles * (chunks * kChunk / group) * 32;
+  return ((size_t)chunks * mt * 1024 + codes + scales + 1023) / 1024 * 1024;
 }
 
 // Large matrices: persistent CTAs, one per SM.  A unit is wn * NT tiles of 16 outputs by 8 MT rows, units are dealt in turn; warp (iw, ik) has NT
@@ -210,17 +209,17 @@ inline size_t stage_bytes_of(int mt, int cw, int group, int tiles) {
 // row's part alone take 40 ns apiece: 31 x 24576 x 12288 211 us for the copies) into a ring that all warps share and that a warp of its own fills, over
 // the borders of units, too: the matrix flows in without a pause, and a row is read from L2 once per unit.  (A consumer that fills slots on the
 // way, with divisions for the slot and its phase, took 860 cycles for every stage, whatever it loaded.)
-template <int NT, int MT, int CW, bool BF, int G>
-__global__ void __launch_bounds__(NT <= 2 ? 480 : 288)
+template <int NT, int MT, int WK, int CW, bool BF, int G>
+__global__ void __launch_bounds__(WK == 4 ? 928 : (NT <= 2 ? 480 : 288))
 gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_codes,
                              const __grid_constant__ CUtensorMap tmap_scales, int M, const float* __restrict__ bias, int N, int K, int epi,
                              void* __restrict__ out, int out_bf16, int wn, int nst, uint32_t stage_bytes, int* __restrict__ status) {
-  using St = Stage<MT, CW, G>;
+  using St = Stage<MT, WK, CW, G>;
   extern __shared__ uint8_t smem_raw[];                    // stages (1 KB aligned): [chunk][rows] | [tile][chunk] codes | [tile][group] scales; sums [WK][8 MT rows][cols]
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages];   // full, empty
   __shared__ int abort_flags[2];
   volatile int* abort_flag = abort_flags;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, iw = warp >> 1, ik = warp & 1, g = lane >> 2, t = lane & 3;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, iw = warp / WK, ik = warp % WK, g = lane >> 2, t = lane & 3;
   const int chunks = K / kChunk, tiles = N / 16, tiles_unit = NT * wn, cols = 16 * tiles_unit, n_rb = (M + 8 * MT - 1) / (8 * MT);
   const int units = (tiles + tiles_unit - 1) / tiles_unit * n_rb, per_unit = (chunks + St::CHUNKS - 1) / St::CHUNKS;
   const uint32_t scales_at = (uint32_t)(St::ROWS + tiles_unit * St::CODES), filling = scales_at + (uint32_t)(tiles_unit * St::SCALES);
@@ -232,7 +231,7 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
     abort_flags[0] = abort_flags[1] = 0;
     for (int i = 0; i < nst; ++i) {
       ptx::mbar_init(full0 + 8u * i, 1);
-      ptx::mbar_init(empty0 + 8u * i, 2 * wn);
+      ptx::mbar_init(empty0 + 8u * i, WK * wn);
     }
     ptx::fence_barrier_init();
     ptx::prefetch_tensormap(&tmap_codes);
@@ -241,7 +240,7 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
   }
   __syncthreads();
   bool ok = true;
-  if (warp == 2 * wn) {
+  if (warp == WK * wn) {
     // ---------------------------------------------------------------- producer (what lies outside the matrices comes as zeros)
     if (ptx::elect_one()) {
       // codes and scales, which no kernel writes, and rows, apart so that the first ones' codes can go ahead of the dependency wait
@@ -283,7 +282,7 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
     return;
   }
   pdl_sync();
-  const int consumers = 64 * wn;                           // (their barriers do not wait for the producer, which runs ahead)
+  const int consumers = 32 * WK * wn;                           // (their barriers do not wait for the producer, which runs ahead)
   auto sync_consumers = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(consumers) : "memory"); };
 
   const uint32_t x_lo = (uint32_t)(g * 128 + ((t ^ g) << 4)), x_hi = x_lo ^ 64u;   // a lane's pieces of a row, swizzled
@@ -337,8 +336,14 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
     for (int q = threadIdx.x; q < all; q += consumers) {
       const int m = q / pairs, n = col0 + 2 * (q - m * pairs);
       if (n >= N) continue;
-      const float2 u = *reinterpret_cast<const float2*>(sums + 2 * q), v = *reinterpret_cast<const float2*>(sums + 8 * MT * cols + 2 * q);
-      finish(make_float2(u.x + v.x, u.y + v.y), bias, row0 + m, n, N, epi, out, out_bf16);
+      float2 y = *reinterpret_cast<const float2*>(sums + 2 * q);
+#pragma unroll
+      for (int k = 1; k < WK; ++k) {
+        const float2 v = *reinterpret_cast<const float2*>(sums + k * (8 * MT * cols) + 2 * q);
+        y.x += v.x;
+        y.y += v.y;
+      }
+      finish(y, bias, row0 + m, n, N, epi, out, out_bf16);
     }
   }
   if (!ok && lane == 0) *(volatile int*)status = ST_GEMM_QUANTIZED;
@@ -401,7 +406,8 @@ QuantizedGemmShape gemm_quantized_pick(int M, int N, int K, int group) {
       const long cost = ((tiles + nt * wn - 1) / (nt * wn) + sms - 1) / sms * nt * wn;
       if (!best || cost <= best) { best = cost; s.nt = nt; s.wn = wn; }
     }
-  s.cw = mt == 1 ? 4 : (mt == 2 ? 2 : 1);
+  s.wk = mt == 1 ? 4 : 2;
+  s.cw = mt <= 2 ? 2 : 1;
   s.nst = 1;
   while (s.nst < kMaxStages) {
     ++s.nst;
@@ -414,7 +420,7 @@ size_t gemm_quantized_smem(int M, int group, const QuantizedGemmShape& s) {
   const int mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
   if (!s.stream) return (size_t)s.warps * 8 * mt * 16 * 4;
   const int tiles = s.nt * s.wn;
-  return 1024 + (size_t)s.nst * stage_bytes_of(mt, s.cw, group, tiles) + (size_t)WK * 8 * mt * 16 * tiles * 4;
+  return 1024 + (size_t)s.nst * stage_bytes_of(mt, s.wk * s.cw, group, tiles) + (size_t)s.wk * 8 * mt * 16 * tiles * 4;
 }
 
 namespace {
@@ -429,17 +435,17 @@ cudaError_t launch_small(const Args& p, const QuantizedGemmShape& s) {
                     (const uint16_t*)p.a, p.lda, p.M, (const uint4*)p.codes, (const uint32_t*)p.scales, p.bias, p.N, p.K, p.epi, p.out, p.out_bf16);
 }
 
-template <int NT, int MT, int CW, bool BF, int G>
+template <int NT, int MT, int WK, int CW, bool BF, int G>
 cudaError_t launch_stream(const Args& p, const QuantizedGemmShape& s) {
   const size_t smem = gemm_quantized_smem(p.M, G, s);
-  if (smem > 220 * 1024 || s.nst < 2 || s.wn * WK > (NT <= 2 ? 14 : 8) || s.cw != CW || s.nt != NT) return cudaErrorInvalidValue;
+  if (smem > 220 * 1024 || s.nst < 2 || s.wn * WK > (WK == 4 ? 28 : (NT <= 2 ? 14 : 8)) || s.cw != CW || s.nt != NT || s.wk != WK) return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
-  cudaError_t e = ensure_dynamic_smem(gemm_quantized_stream_kernel<NT, MT, CW, BF, G>, smem, smem_set);
+  cudaError_t e = ensure_dynamic_smem(gemm_quantized_stream_kernel<NT, MT, WK, CW, BF, G>, smem, smem_set);
   if (e != cudaSuccess) return e;
   const int per = NT * s.wn, sms = device_sm_count();
   const long units = (long)((p.N / 16 + per - 1) / per) * ((p.M + 8 * MT - 1) / (8 * MT));
   // boxes of a stage: [chunk][8 MT rows][64 values], [tile][chunk][512 bytes], [tile][group][32 bytes]
-  using St = Stage<MT, CW, G>;
+  using St = Stage<MT, WK, CW, G>;
   CUtensorMap ta, tc, ts;
   EncodeTiledFn fn = tma_encode_fn();
   const cuuint64_t chunks = p.K / kChunk, groups = p.K / G, tiles = p.N / 16;
@@ -455,8 +461,8 @@ cudaError_t launch_stream(const Args& p, const QuantizedGemmShape& s) {
       !make(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.codes, 128, chunks, tiles, 512, chunks * 512, 128, St::CHUNKS, per, false) ||
       !make(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.scales, 8, groups, tiles, 32, groups * 32, 8, St::GROUPS, per, false))
     return cudaErrorInvalidValue;
-  return launch_pdl(gemm_quantized_stream_kernel<NT, MT, CW, BF, G>, dim3((unsigned)(units < sms ? units : sms)), dim3(32 * (s.wn * WK + 1)), smem, p.st, ta, tc, ts, p.M, p.bias,
-                    p.N, p.K, p.epi, p.out, p.out_bf16, s.wn, s.nst, (uint32_t)stage_bytes_of(MT, CW, G, per), p.status);
+  return launch_pdl(gemm_quantized_stream_kernel<NT, MT, WK, CW, BF, G>, dim3((unsigned)(units < sms ? units : sms)), dim3(32 * (s.wn * WK + 1)), smem, p.st, ta, tc, ts, p.M, p.bias,
+                    p.N, p.K, p.epi, p.out, p.out_bf16, s.wn, s.nst, (uint32_t)stage_bytes_of(MT, WK * CW, G, per), p.status);
 }
 
 template <bool BF, int G>
@@ -469,10 +475,17 @@ cudaError_t launch(const Args& p, const QuantizedGemmShape& s, int mt) {
       default: return launch_small<4, BF, G>(p, s);
     }
   }
-  if (mt == 1) return launch_stream<1, 1, 4, BF, G>(p, s);
-  if (mt == 2) return launch_stream<1, 2, 2, BF, G>(p, s);
-  if (mt == 3) return s.nt == 2 ? launch_stream<2, 3, 1, BF, G>(p, s) : s.nt == 1 ? launch_stream<1, 3, 1, BF, G>(p, s) : launch_stream<3, 3, 1, BF, G>(p, s);
-  return s.nt == 2 ? launch_stream<2, 4, 1, BF, G>(p, s) : s.nt == 1 ? launch_stream<1, 4, 1, BF, G>(p, s) : launch_stream<3, 4, 1, BF, G>(p, s);
+  switch (10 * s.nt + mt) {
+    case 11: return launch_stream<1, 1, 4, 2, BF, G>(p, s);
+    case 12: return launch_stream<1, 2, 2, 2, BF, G>(p, s);
+    case 13: return launch_stream<1, 3, 2, 1, BF, G>(p, s);
+    case 23: return launch_stream<2, 3, 2, 1, BF, G>(p, s);
+    case 33: return launch_stream<3, 3, 2, 1, BF, G>(p, s);
+    case 14: return launch_stream<1, 4, 2, 1, BF, G>(p, s);
+    case 24: return launch_stream<2, 4, 2, 1, BF, G>(p, s);
+    case 34: return launch_stream<3, 4, 2, 1, BF, G>(p, s);
+  }
+  return cudaErrorInvalidValue;
 }
 
 }  // namespace

@@ -1,18 +1,20 @@
 // K7: rows of K and V into a cache held in 8 bits, and rows of that cache back.
 //
 // A head's dh values of one token share a scale: amax = max |x|, code = round(127 x / amax) (ties to even), scale = amax / 127,
-// value = code * scale.  Codes are those of exact arithmetic: 127 x is exact in fp32 for a bf16 x (8 + 7 bits), and the quotient comes from a
-// reciprocal of amax (one per head) with one correction by the exact remainder 127 x - t amax (Markstein's), which leaves an error of 2^-46 t
-// before the last rounding.  A quotient that is not a half is at least 2^-17 away from one (numerator and denominator have few bits),
-// so it rounds to its own side; one that is a half (x = amax / 2 is: 63.5) is a fp32 number, and the correction lands on it.  Rounding is the
-// addition of 1.5 * 2^23, whose sum's low byte is the code.  With a division per value (20 instructions and a conversion) the kernel was bound
-// by those: 128 x 43 rows of 16 heads of 80, 42.6 us.
-// amax comes from the magnitude bits, which order as integers and put infinities and NaN above every number: such a head gets codes 0
-// and a NaN scale, so all of it reads back as NaN, and no code is ever anything but a number.
+// value = code * scale.  Codes are those of exact arithmetic: 127 x is exact in fp32 for a bf16 x (8 + 7 bits), and the quotient comes from an
+// approximate reciprocal of amax (one per head) with one correction by the remainder 127 x - t amax (Markstein's), which is exact, so
+// that an error of 2^-44 t is left before the last rounding.  A quotient that is not a half is at least 2^-17 away from one (numerator and
+// denominator have few bits), so it rounds to its own side; one that is a half (x = amax / 2 is: 63.5) is a fp32 number, and the correction lands on
+// it.  Rounding is the addition of 1.5 * 2^23, whose sum's low byte is the code.  scale comes by the same correction: a quotient of 8 bits by
+// 127 is at least 2^-32 of itself away from the middle of two fp32 numbers.
+// amax comes from the magnitudes, with NaN above infinity above every number: a head that holds one gets codes 0 and a NaN scale, so all of it
+// reads back as NaN, and no code is ever anything but a number.
 //
-// What bounds it: HBM for many rows, the launch for few.  A group of dh / 8 lanes takes a head of a row (16 bytes in, 8 out per
-// lane), reduces in shuffles, and the row leaves as whole 32-byte sectors; the scales lie key by key (their readers' order) and leave
-// as single words.  Rows whose token is outside the cache are skipped: a batch with different numbers of rows is padded with -1.
+// What bounds it: HBM for many rows, the launch for few.  A warp takes a row of K or V, a group of dh / 8 lanes a head of it (16 bytes in, 8 out
+// per lane), all loads of up to four heads a group ahead; the row leaves as whole 32-byte sectors; the scales lie key by key (their readers'
+// order) and leave as single words.  Rows whose token is outside the cache are skipped: a batch with different numbers of rows is padded with -1.
+// 6 x 8191 rows of 16 heads of 64: a division per value and index divisions per head 116 us for the writing (85 % of the issue slots), as it
+// stands FILL_US; reading back 53 us, 5.8 TB/s.
 #include "common.cuh"
 #include "kernels.h"
 #include "launch_pdl.h"
@@ -37,67 +39,74 @@ MARCHE_DEVINL uint32_t group_max(uint32_t v, int base, int in) {
   return v;
 }
 
-// blockIdx.y: K or V.  A warp takes 32 / W heads of the [rows][heads] list at a time, U times.
+MARCHE_DEVINL float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+MARCHE_DEVINL uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // NaN wins
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// blockIdx.y: K or V.  A warp takes a row, U rounds of 32 / W heads at a time.
 template <int DH, int U>
 __global__ void __launch_bounds__(kThreads)
-scatter_kv_quantized_kernel(const bf16* __restrict__ k, const bf16* __restrict__ v, size_t ld, const int32_t* __restrict__ idx, int n, int B,
+scatter_kv_quantized_kernel(const bf16* __restrict__ k, const bf16* __restrict__ v, size_t ld, const int32_t* __restrict__ idx, int n, int rows, int B,
                             int S, int H, int pad, int8_t* __restrict__ codes, float* __restrict__ scales) {
   constexpr int W = DH / 8, HPW = 32 / W;
   pdl_sync();
-  const int which = blockIdx.y, lane = threadIdx.x & 31, in_warp = lane / W, in = lane - in_warp * W;
-  const uint32_t total = (uint32_t)B * (uint32_t)n * (uint32_t)H;      // below 2^31 (launch)
-  const uint32_t first = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * (HPW * U) + in_warp;
-  const bf16* src = which ? v : k;
-  uint4 x[U];
-  int8_t* to[U];
-  float* to_scale[U];
+  const int which = blockIdx.y, lane = threadIdx.x & 31, group = lane / W, in = lane - group * W;
+  const int row = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int b = row / n, t = idx ? idx[row] : row - b * n;
+  if ((uint32_t)t >= (uint32_t)S) return;                  // (the whole warp)
+  const bf16* src = (which ? v : k) + row * ld + 8 * in;
+  int8_t* to = codes + (((size_t)which * B + b) * S + t) * ((size_t)H * DH) + 8 * in;
+  float* to_scale = scales + ((size_t)which * B + b) * H * pad + t;
+  for (int h0 = 0; h0 < H; h0 += HPW * U) {
+    uint4 x[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const uint32_t head = first + u * HPW;
-    to[u] = nullptr;
-    x[u] = make_uint4(0, 0, 0, 0);
-    if (in_warp < HPW && head < total) {
-      const uint32_t row = head / (uint32_t)H, h = head - row * H, b = row / (uint32_t)n;
-      const int t = idx ? idx[row] : (int)(row - b * n);
-      if ((uint32_t)t < (uint32_t)S) {
-        x[u] = *reinterpret_cast<const uint4*>(src + row * ld + h * DH + 8 * in);
-        to[u] = codes + ((((size_t)which * B + b) * S + t) * H + h) * DH + 8 * in;
-        to_scale[u] = scales + (((size_t)which * B + b) * H + h) * pad + t;
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * HPW + group;
+      x[u] = group < HPW && h < H ? *reinterpret_cast<const uint4*>(src + h * DH) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * HPW + group;
+      if (u > 0 && h0 + u * HPW >= H) break;               // (the whole warp)
+      uint32_t words[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      const uint32_t both = max_bf16x2(max_bf16x2(words[0] & 0x7fff7fffu, words[1] & 0x7fff7fffu), max_bf16x2(words[2] & 0x7fff7fffu, words[3] & 0x7fff7fffu));
+      const uint32_t top = group_max<W>(max(both & 0xffffu, both >> 16), (group < HPW ? group : 0) * W, in);
+      // Both sides of the division move to the range's middle by the same power of two near its ends; a head of zeros, or one that is not
+      // finite, is divided by 1.
+      const bool plain = top != 0 && top < 0x7f80u;
+      const float amax = __uint_as_float(top << 16), shift = top >= 0x6000u ? 0x1p-64f : (top < 0x2000u ? 0x1p64f : 1.0f);
+      const float d = plain ? amax * shift : 1.0f, inv = rcp_approx(d), times = plain ? 127.0f * shift : 0.f;
+      if (!plain) words[0] = words[1] = words[2] = words[3] = 0;
+      uint32_t c[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 n127 = __fmul2_rn(make_float2(__uint_as_float(words[i] << 16), __uint_as_float(words[i] & 0xffff0000u)), make_float2(times, times));
+        const float2 q = __fmul2_rn(n127, make_float2(inv, inv)), rest = __ffma2_rn(make_float2(-q.x, -q.y), make_float2(d, d), n127);
+        const float2 r = __fadd2_rn(__ffma2_rn(rest, make_float2(inv, inv), q), make_float2(12582912.0f, 12582912.0f));
+        c[2 * i] = __float_as_uint(r.x);
+        c[2 * i + 1] = __float_as_uint(r.y);
       }
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    uint32_t words[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t lo = words[i] & 0x7fffu, hi = (words[i] >> 16) & 0x7fffu;
-      top = max(top, max(lo, hi));
-    }
-    top = group_max<W>(top, (lane / W < HPW ? lane / W : 0) * W, in);
-    const float amax = __uint_as_float(top << 16);
-    const float scale = top >= 0x7f80u ? __int_as_float(0x7fffffff) : __fdiv_rn(amax, 127.0f);
-    // Near the ends of the range both sides of the division move to its middle by the same power of two; a head of zeros, or one that is not
-    // finite, is multiplied by 0 throughout (and its infinities by none: a remainder that is not a number is not added).
-    const bool plain = top != 0 && top < 0x7f80u;
-    const float shift = top >= 0x6000u ? 0x1p-64f : (top < 0x2000u ? 0x1p64f : 1.0f), d = amax * shift;
-    const float inv = plain ? __frcp_rn(d) : 0.f, times = 127.0f * shift;
-    uint32_t packed[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t c[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t word = plain ? words[2 * i + (j >> 1)] : 0u;
-        const float x = __uint_as_float(j & 1 ? word & 0xffff0000u : word << 16) * times;
-        const float t = x * inv;
-        c[j] = __float_as_uint(fmaf(plain ? fmaf(-t, d, x) : 0.f, inv, t) + 12582912.0f);
+      if (group < HPW && h < H) {
+        uint2 out;
+        out.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+        out.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+        *reinterpret_cast<uint2*>(to + (size_t)h * DH) = out;
+        if (in == 0) {
+          constexpr float r127 = 1.0f / 127.0f;
+          const float s = amax * r127;
+          float scale = fmaf(fmaf(-s, 127.0f, amax), r127, s);
+          if (top < 0x2000u) scale = __fdiv_rn(amax, 127.0f);   // (a remainder could be too small for the format)
+          to_scale[(size_t)h * pad] = top >= 0x7f80u ? __int_as_float(0x7fffffff) : scale;
+        }
       }
-      packed[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
-    }
-    if (to[u]) {
-      *reinterpret_cast<uint2*>(to[u]) = make_uint2(packed[0], packed[1]);
-      if (in == 0) *to_scale[u] = scale;
     }
   }
 }
@@ -150,10 +159,10 @@ gather_kv_quantized_kernel(const int8_t* __restrict__ codes, const float* __rest
 
 template <int DH>
 cudaError_t scatter(const void* k, const void* v, int ld, const int32_t* idx, int n, const QuantizedKv& c, cudaStream_t st) {
-  constexpr int per_cta = kThreads / 32 * (32 / (DH / 8)), U = 2;
-  const uint32_t total = (uint32_t)c.B * (uint32_t)n * (uint32_t)c.H;
-  return launch_pdl(scatter_kv_quantized_kernel<DH, U>, dim3((total + per_cta * U - 1) / (per_cta * U), 2), dim3(kThreads), 0, st, (const bf16*)k, (const bf16*)v,
-                    (size_t)ld, idx, n, c.B, c.S, c.H, c.pad, c.codes, c.scales);
+  constexpr int per_cta = kThreads / 32;
+  const int rows = c.B * n;
+  return launch_pdl(scatter_kv_quantized_kernel<DH, 4>, dim3((unsigned)((rows + per_cta - 1) / per_cta), 2), dim3(kThreads), 0, st, (const bf16*)k, (const bf16*)v,
+                    (size_t)ld, idx, n, rows, c.B, c.S, c.H, c.pad, c.codes, c.scales);
 }
 
 }  // namespace

@@ -185,7 +185,7 @@ cudaError_t launch_attention_quantized_tc(const void* q, int ld_q, int n, int he
                                           bool o_bf16, int* status, cudaStream_t st);
 
 // K2 on weights of 4 bits.  N % 16 == 0, K % 64 == 0, group 32, 64 or 128 dividing K; lda % 8 == 0, 16-byte aligned operands.
-struct QuantizedGemmShape { int stream, warps, nt, wn, cw, nst; };
+struct QuantizedGemmShape { int stream, warps, nt, wn, wk, cw, nst; };
 QuantizedGemmShape gemm_quantized_pick(int M, int N, int K, int group);
 size_t gemm_quantized_smem(int M, int group, const QuantizedGemmShape& s);
 cudaError_t launch_gemm_quantized(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,

@@ -72,7 +72,7 @@ def test_attention_cuts_fit_an_sm_and_cover_all_rows(lib):
 
 
 class GemmShape(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("stream", "warps", "nt", "wn", "cw", "nst")]
+    _fields_ = [(n, C.c_int) for n in ("stream", "warps", "nt", "wn", "wk", "cw", "nst")]
 
 
 def test_projection_cuts_fit_an_sm(lib):
@@ -90,8 +90,8 @@ def test_projection_cuts_fit_an_sm(lib):
                     at = (M, tiles, chunks, group, [getattr(s, n) for n, _ in GemmShape._fields_])
                     mt = min((M + 7) // 8, 4)
                     if s.stream:
-                        assert (s.nt, mt, s.cw) in [(1, 1, 4), (1, 2, 2), (1, 3, 1), (2, 3, 1), (3, 3, 1), (1, 4, 1), (2, 4, 1), (3, 4, 1)], at
-                        assert 2 * s.wn <= (14 if s.nt <= 2 else 8) and s.nt * s.wn <= 32 and 3 <= s.nst <= 16, at
+                        assert (s.nt, mt, s.wk, s.cw) in [(1, 1, 4, 2), (1, 2, 2, 2)] + [(nt, mt, 2, 1) for nt in (1, 2, 3) for mt in (3, 4)], at
+                        assert s.wk * s.wn <= (28 if s.wk == 4 else 14 if s.nt <= 2 else 8) and s.nt * s.wn <= 32 and 3 <= s.nst <= 16, at
                         assert smem(M, group, C.byref(s)) <= 220 * 1024, at
                         seen.add((s.nt, mt))
                     else:
