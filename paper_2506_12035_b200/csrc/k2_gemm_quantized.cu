@@ -194,35 +194,34 @@ gemm_quantized_small_kernel(const uint16_t* __restrict__ a, int lda, int M, cons
 constexpr int kMaxStages = 16;
 enum { ST_GEMM_QUANTIZED = 0x66 };
 
-// Of a stage: WK CW chunks of the rows (a chunk's 128 bytes under TMA's 128-byte swizzle, eight rows 1 KB), of the unit's tiles, and their scales.
-template <int MT, int WK, int CW, int G> struct Stage {
-  static constexpr int CHUNKS = WK * CW, GROUPS = CHUNKS * kChunk / G, ROWS = CHUNKS * MT * 1024, CODES = CHUNKS * 512, SCALES = GROUPS * 32;
-  static_assert(CHUNKS * kChunk % G == 0, "whole groups");
+// Of a stage: WK CW chunks of the eight rows (a chunk's 128 bytes under TMA's 128-byte swizzle), of the unit's tiles, and their scales.
+constexpr int WK = 4, CW = 2, kStageChunks = WK * CW, kMaxTiles = 7;
+template <int G> struct Stage {
+  static constexpr int GROUPS = kStageChunks * kChunk / G, ROWS = kStageChunks * 1024, CODES = kStageChunks * 512, SCALES = GROUPS * 32;
 };
-inline size_t stage_bytes_of(int mt, int chunks, int group, int tiles) {
-  const size_t codes = (size_t)tiles * chunks * 512, scales = (size_t)tiles * (chunks * kChunk / group) * 32;
-  return ((size_t)chunks * mt * 1024 + codes + scales + 1023) / 1024 * 1024;
+inline size_t stage_bytes_of(int group, int tiles) {
+  return ((size_t)kStageChunks * 1024 + (size_t)tiles * (kStageChunks * 512 + kStageChunks * kChunk / group * 32) + 1023) / 1024 * 1024;
 }
 
-// Large matrices: persistent CTAs, one per SM.  A unit is wn * NT tiles of 16 outputs by 8 MT rows, units are dealt in turn; warp (iw, ik) has NT
-// of the tiles and every second group of CW chunks.  Codes, scales and rows of a stage come by one TMA box each (bulk copies of a tile's or a
+// Large matrices, up to eight rows: persistent CTAs, one per SM.  A unit is wn tiles of 16 outputs, units are dealt in turn; warp (iw, ik) has one
+// of the tiles and the ik-th CW chunks of every stage.  Codes, scales and rows of a stage come by one TMA box each (bulk copies of a tile's or a
 // row's part alone take 40 ns apiece: 31 x 24576 x 12288 211 us for the copies) into a ring that all warps share and that a warp of its own fills, over
-// the borders of units, too: the matrix flows in without a pause, and a row is read from L2 once per unit.  (A consumer that fills slots on the
-// way, with divisions for the slot and its phase, took 860 cycles for every stage, whatever it loaded.)
-template <int NT, int MT, int WK, int CW, bool BF, int G>
-__global__ void __launch_bounds__(WK == 4 ? 928 : (NT <= 2 ? 480 : 288))
+// the borders of units, too: the matrix flows in without a pause.  (A consumer that fills slots on the way, with divisions for the slot and its
+// phase, took 860 cycles for every stage, whatever it loaded.)  1 x 16384 x 8192: two warps along K 22.7 us, four 20.9, of 11.0 for the bytes; the
+// launch and the first stage's way take 4.
+template <bool BF, int G>
+__global__ void __launch_bounds__(32 * (WK * kMaxTiles + 1))
 gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_codes,
                              const __grid_constant__ CUtensorMap tmap_scales, int M, const float* __restrict__ bias, int N, int K, int epi,
                              void* __restrict__ out, int out_bf16, int wn, int nst, uint32_t stage_bytes, int* __restrict__ status) {
-  using St = Stage<MT, WK, CW, G>;
-  extern __shared__ uint8_t smem_raw[];                    // stages (1 KB aligned): [chunk][rows] | [tile][chunk] codes | [tile][group] scales; sums [WK][8 MT rows][cols]
+  using St = Stage<G>;
+  extern __shared__ uint8_t smem_raw[];                    // stages (1 KB aligned): [chunk][rows] | [tile][chunk] codes | [tile][group] scales; sums [WK][8 rows][cols]
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages];   // full, empty
   __shared__ int abort_flags[2];
   volatile int* abort_flag = abort_flags;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, iw = warp / WK, ik = warp % WK, g = lane >> 2, t = lane & 3;
-  const int chunks = K / kChunk, tiles = N / 16, tiles_unit = NT * wn, cols = 16 * tiles_unit, n_rb = (M + 8 * MT - 1) / (8 * MT);
-  const int units = (tiles + tiles_unit - 1) / tiles_unit * n_rb, per_unit = (chunks + St::CHUNKS - 1) / St::CHUNKS;
-  const uint32_t scales_at = (uint32_t)(St::ROWS + tiles_unit * St::CODES), filling = scales_at + (uint32_t)(tiles_unit * St::SCALES);
+  const int chunks = K / kChunk, cols = 16 * wn, units = (N / 16 + wn - 1) / wn, per_unit = (chunks + kStageChunks - 1) / kStageChunks;
+  const uint32_t scales_at = (uint32_t)(St::ROWS + wn * St::CODES), filling = scales_at + (uint32_t)(wn * St::SCALES);
   const uint32_t raw = ptx::smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u, full0 = ptx::smem_u32(bars), empty0 = full0 + 8u * kMaxStages;
   const uint8_t* smem = smem_raw + (ring - raw);
   float* sums = reinterpret_cast<float*>(smem_raw + (ring - raw) + (size_t)nst * stage_bytes);
@@ -247,26 +246,22 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
       auto load_codes = [&](int slot, int tile0, int piece) {
         const uint32_t dst = ring + (uint32_t)slot * stage_bytes, bar = full0 + 8u * slot;
         ptx::mbar_expect_tx(bar, filling);
-        ptx::tma_load_3d(dst + St::ROWS, &tmap_codes, 0, piece * St::CHUNKS, tile0, bar);
+        ptx::tma_load_3d(dst + St::ROWS, &tmap_codes, 0, piece * kStageChunks, tile0, bar);
         ptx::tma_load_3d(dst + scales_at, &tmap_scales, 0, piece * St::GROUPS, tile0, bar);
       };
-      auto load_rows = [&](int slot, int row0, int piece) {
-        ptx::tma_load_3d(ring + (uint32_t)slot * stage_bytes, &tmap_a, 0, row0, piece * St::CHUNKS, full0 + 8u * slot);
+      auto load_rows = [&](int slot, int piece) {
+        ptx::tma_load_3d(ring + (uint32_t)slot * stage_bytes, &tmap_a, 0, 0, piece * kStageChunks, full0 + 8u * slot);
       };
       const int ahead = min(nst, per_unit);                // of the first unit's
-      {
-        const int tile0 = (int)blockIdx.x / n_rb * tiles_unit, row0 = (int)blockIdx.x % n_rb * (8 * MT);
-        for (int i = 0; i < ahead; ++i) load_codes(i, tile0, i);
-        pdl_wait();
-        for (int i = 0; i < ahead; ++i) load_rows(i, row0, i);
-      }
+      for (int i = 0; i < ahead; ++i) load_codes(i, (int)blockIdx.x * wn, i);
+      pdl_wait();
+      for (int i = 0; i < ahead; ++i) load_rows(i, i);
       int slot = ahead == nst ? 0 : ahead, phase = ahead == nst ? 0 : 1, filled = ahead;   // phase: parity of the emptying waited for (1: a fresh slot passes)
       for (int unit = blockIdx.x, first = ahead; unit < units && ok; unit += gridDim.x, first = 0) {
-        const int tile0 = unit / n_rb * tiles_unit, row0 = unit % n_rb * (8 * MT);
         for (int p = first; p < per_unit; ++p) {
           if (!ptx::mbar_wait(empty0 + 8u * slot, (uint32_t)phase, abort_flag)) { ok = false; break; }
-          load_codes(slot, tile0, p);
-          load_rows(slot, row0, p);
+          load_codes(slot, unit * wn, p);
+          load_rows(slot, p);
           ++filled;
           if (++slot == nst) { slot = 0; phase ^= 1; }
         }
@@ -282,68 +277,54 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
     return;
   }
   pdl_sync();
-  const int consumers = 32 * WK * wn;                           // (their barriers do not wait for the producer, which runs ahead)
+  const int consumers = 32 * WK * wn;                      // (their barriers do not wait for the producer, which runs ahead)
   auto sync_consumers = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(consumers) : "memory"); };
 
   const uint32_t x_lo = (uint32_t)(g * 128 + ((t ^ g) << 4)), x_hi = x_lo ^ 64u;   // a lane's pieces of a row, swizzled
   int slot = 0, phase = 0;
   for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int row0 = (unit % n_rb) * (8 * MT), col0 = unit / n_rb * cols;
-    float acc[NT][MT][4];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int m = 0; m < MT; ++m) acc[i][m][0] = acc[i][m][1] = acc[i][m][2] = acc[i][m][3] = 0.f;
+    float acc[1][4] = {};
     for (int p = 0; p < per_unit && ok; ++p) {
       if (!__all_sync(0xffffffffu, ptx::mbar_wait(full0 + 8u * slot, (uint32_t)phase, abort_flag))) { ok = false; break; }
       const uint8_t* stage = smem + (uint32_t)slot * stage_bytes;
-      const uint8_t* w_at = stage + St::ROWS + iw * NT * St::CODES + lane * 16;
-      const uint8_t* s_at = stage + scales_at + iw * NT * St::SCALES + g * 4;
-      const int left = chunks - p * St::CHUNKS;
+      const uint8_t* w_at = stage + St::ROWS + iw * St::CODES + lane * 16;
+      const uint8_t* s_at = stage + scales_at + iw * St::SCALES + g * 4;
+      const int left = chunks - p * kStageChunks;
 #pragma unroll
       for (int j = 0; j < CW; ++j) {
         const int c = ik * CW + j;                         // of the stage
         if (c < left) {
-          uint4 x[MT][2];
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            x[m][0] = *reinterpret_cast<const uint4*>(stage + x_lo + (c * MT + m) * 1024);
-            x[m][1] = *reinterpret_cast<const uint4*>(stage + x_hi + (c * MT + m) * 1024);
-          }
-#pragma unroll
-          for (int i = 0; i < NT; ++i)
-            multiply_chunk<MT, BF, G>(acc[i], *reinterpret_cast<const uint4*>(w_at + i * St::CODES + c * 512), x, [&](int k) {
-              return *reinterpret_cast<const uint32_t*>(s_at + i * St::SCALES + (G == 32 ? 2 * c + k : c * kChunk / G) * 32);
-            });
+          uint4 x[1][2];
+          x[0][0] = *reinterpret_cast<const uint4*>(stage + x_lo + c * 1024);
+          x[0][1] = *reinterpret_cast<const uint4*>(stage + x_hi + c * 1024);
+          multiply_chunk<1, BF, G>(acc, *reinterpret_cast<const uint4*>(w_at + c * 512), x, [&](int k) {
+            return *reinterpret_cast<const uint32_t*>(s_at + (G == 32 ? 2 * c + k : c * kChunk / G) * 32);
+          });
         }
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(empty0 + 8u * slot);
       if (++slot == nst) { slot = 0; phase ^= 1; }
     }
-    // accumulator: outputs g and g + 8, rows 2 t and 2 t + 1 of an eight
+    // accumulator: outputs g and g + 8, rows 2 t and 2 t + 1
     sync_consumers();                                      // the unit before has been stored
-    float* mine = sums + ik * (8 * MT * cols) + 16 * NT * iw;
+    float* mine = sums + ik * (8 * cols) + 16 * iw;
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * cols + 16 * i + g + 8 * (e >> 1)] = acc[i][m][e];
+    for (int e = 0; e < 4; ++e) mine[(2 * t + (e & 1)) * cols + g + 8 * (e >> 1)] = acc[0][e];
     sync_consumers();
     if (*abort_flag) { ok = false; continue; }             // nothing is stored of what is missing; the barriers stay in step
-    const int pairs = cols / 2, all = min(8 * MT, M - row0) * pairs;   // two neighbouring outputs of a row each
+    const int pairs = cols / 2, all = M * pairs;           // two neighbouring outputs of a row each
     for (int q = threadIdx.x; q < all; q += consumers) {
-      const int m = q / pairs, n = col0 + 2 * (q - m * pairs);
+      const int m = q / pairs, n = unit * cols + 2 * (q - m * pairs);
       if (n >= N) continue;
       float2 y = *reinterpret_cast<const float2*>(sums + 2 * q);
 #pragma unroll
       for (int k = 1; k < WK; ++k) {
-        const float2 v = *reinterpret_cast<const float2*>(sums + k * (8 * MT * cols) + 2 * q);
+        const float2 v = *reinterpret_cast<const float2*>(sums + k * (8 * cols) + 2 * q);
         y.x += v.x;
         y.y += v.y;
       }
-      finish(y, bias, row0 + m, n, N, epi, out, out_bf16);
+      finish(y, bias, m, n, N, epi, out, out_bf16);
     }
   }
   if (!ok && lane == 0) *(volatile int*)status = ST_GEMM_QUANTIZED;
@@ -353,7 +334,7 @@ gemm_quantized_stream_kernel(const __grid_constant__ CUtensorMap tmap_a, const _
 __global__ void __launch_bounds__(128)
 quantize_weights_kernel(const float* __restrict__ w, int N, int K, int group, uint32_t* __restrict__ codes, uint16_t* __restrict__ scales) {
   __shared__ float s_scale[16][2];
-  pdl_sync();
+  pdl_wait();                                              // (and no early release: see the end)
   const int span = group > kChunk ? group : kChunk, per = span / 8, r = threadIdx.x >> 3, j = threadIdx.x & 7;
   const int tile = blockIdx.x, k0 = blockIdx.y * span;
   const float* src = w + (size_t)(tile * 16 + r) * K + k0 + j * per;
@@ -386,41 +367,45 @@ quantize_weights_kernel(const float* __restrict__ w, int N, int K, int group, ui
     }
     codes[(((size_t)tile * (K / kChunk) + k0 / kChunk + c) * 32 + lane) * 4 + s] = word;
   }
+  // A projection fetches its first codes ahead of its dependency wait: it may not start before these are written and visible.
+  __threadfence();
 }
 
 }  // namespace
 
-// How a projection is cut.  stream false: warps of a CTA of the kernel for small matrices.  Else tiles of a warp, warps along the outputs, stages.
+// How a projection is cut: the kernel for small matrices, with so many warps per CTA; for large ones the one for up to eight rows, with units of wn
+// tiles and nst stages, or, for more, the one on tcgen05 by CTAs or pairs of them.
+// Large: the matrix is worth a ring and the CTAs are many enough to fill the device, which few outputs with a long K are only as pairs (us, small
+// kernel and tcgen05: 31 x 4096 x 11008 20.0, 16.7; 31 x 8192 x 4096 15.0, 11.8; 31 x 16384 x 1024 11.6, 8.4; but 31 x 4096 x 4096 8.7, 9.4;
+// 31 x 8192 x 1024 6.8, 7.5; 31 x 1024 x 8192 8.7, 13.1; 1 x 16384 x 8192 on tcgen05 21.3, by the ring 20.9).
 QuantizedGemmShape gemm_quantized_pick(int M, int N, int K, int group) {
-  const int tiles = N / 16, chunks = K / kChunk, sms = device_sm_count(), mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
+  const int tiles = N / 16, chunks = K / kChunk, sms = device_sm_count();
   QuantizedGemmShape s = {};
-  s.stream = tiles >= 2 * sms && (long)tiles * chunks >= 64L * sms;
-  if (!s.stream) {
-    s.warps = chunks < 8 ? chunks : (tiles <= sms && chunks >= 16 ? 16 : 8);
-    return s;
-  }
-  // the fewest tiles in turn on an SM
-  long best = 0;
-  for (int nt = 1; nt <= (mt >= 3 ? 3 : 1); ++nt)
-    for (int wn = 4; wn <= (nt <= 2 ? 7 : 4); ++wn) {
-      const long cost = ((tiles + nt * wn - 1) / (nt * wn) + sms - 1) / sms * nt * wn;
-      if (!best || cost <= best) { best = cost; s.nt = nt; s.wn = wn; }
+  const long size = (long)tiles * chunks;
+  if (M > 8) {
+    // a unit is 128 outputs by 16 or 32 rows; pairs where half the stages (of 4 chunks) in more turns are fewer
+    const int nr = M <= 16 ? 16 : 32, stages = (chunks + 3) / 4;
+    const long units = (long)((N + 127) / 128) * ((M + nr - 1) / nr);
+    if (size >= (tiles >= 2 * sms ? 64L : 128L) * sms && 6 * units >= sms)
+      s.tc = stages >= 2 && (units + sms / 2 - 1) / (sms / 2) * ((stages + 1) / 2) < (units + sms - 1) / sms * stages ? 2 : 1;
+  } else if (tiles >= 2 * sms && size >= 64L * sms) {
+    long best = 0;                                         // the fewest tiles in turn on an SM
+    for (int wn = 4; wn <= kMaxTiles; ++wn) {
+      const long cost = ((tiles + wn - 1) / wn + sms - 1) / sms * wn;
+      if (!best || cost <= best) { best = cost; s.wn = wn; }
     }
-  s.wk = mt == 1 ? 4 : 2;
-  s.cw = mt <= 2 ? 2 : 1;
-  s.nst = 1;
-  while (s.nst < kMaxStages) {
-    ++s.nst;
-    if (gemm_quantized_smem(M, group, s) > 200 * 1024) { --s.nst; break; }
+    while (s.nst < kMaxStages) {
+      ++s.nst;
+      if (gemm_quantized_smem(M, group, s) > 200 * 1024) { --s.nst; break; }
+    }
   }
+  if (!s.tc && !s.wn) s.warps = chunks < 8 ? chunks : (tiles <= sms && chunks >= 16 ? 16 : 8);
   return s;
 }
 
 size_t gemm_quantized_smem(int M, int group, const QuantizedGemmShape& s) {
-  const int mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
-  if (!s.stream) return (size_t)s.warps * 8 * mt * 16 * 4;
-  const int tiles = s.nt * s.wn;
-  return 1024 + (size_t)s.nst * stage_bytes_of(mt, s.wk * s.cw, group, tiles) + (size_t)s.wk * 8 * mt * 16 * tiles * 4;
+  if (s.wn) return 1024 + (size_t)s.nst * stage_bytes_of(group, s.wn) + (size_t)WK * 8 * 16 * s.wn * 4;
+  return (size_t)s.warps * 8 * (M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8) * 16 * 4;
 }
 
 namespace {
@@ -435,17 +420,15 @@ cudaError_t launch_small(const Args& p, const QuantizedGemmShape& s) {
                     (const uint16_t*)p.a, p.lda, p.M, (const uint4*)p.codes, (const uint32_t*)p.scales, p.bias, p.N, p.K, p.epi, p.out, p.out_bf16);
 }
 
-template <int NT, int MT, int WK, int CW, bool BF, int G>
+template <bool BF, int G>
 cudaError_t launch_stream(const Args& p, const QuantizedGemmShape& s) {
   const size_t smem = gemm_quantized_smem(p.M, G, s);
-  if (smem > 220 * 1024 || s.nst < 2 || s.wn * WK > (WK == 4 ? 28 : (NT <= 2 ? 14 : 8)) || s.cw != CW || s.nt != NT || s.wk != WK) return cudaErrorInvalidValue;
+  if (smem > 220 * 1024 || s.nst < 2 || s.wn > kMaxTiles || p.M > 8) return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
-  cudaError_t e = ensure_dynamic_smem(gemm_quantized_stream_kernel<NT, MT, WK, CW, BF, G>, smem, smem_set);
+  cudaError_t e = ensure_dynamic_smem(gemm_quantized_stream_kernel<BF, G>, smem, smem_set);
   if (e != cudaSuccess) return e;
-  const int per = NT * s.wn, sms = device_sm_count();
-  const long units = (long)((p.N / 16 + per - 1) / per) * ((p.M + 8 * MT - 1) / (8 * MT));
-  // boxes of a stage: [chunk][8 MT rows][64 values], [tile][chunk][512 bytes], [tile][group][32 bytes]
-  using St = Stage<MT, WK, CW, G>;
+  const int sms = device_sm_count(), units = (p.N / 16 + s.wn - 1) / s.wn;
+  // boxes of a stage: [chunk][8 rows][64 values], [tile][chunk][512 bytes], [tile][group][32 bytes]
   CUtensorMap ta, tc, ts;
   EncodeTiledFn fn = tma_encode_fn();
   const cuuint64_t chunks = p.K / kChunk, groups = p.K / G, tiles = p.N / 16;
@@ -457,35 +440,23 @@ cudaError_t launch_stream(const Args& p, const QuantizedGemmShape& s) {
                     swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
-  if (!make(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.a, kChunk, p.M, chunks, (cuuint64_t)p.lda * 2, kChunk * 2, kChunk, 8 * MT, St::CHUNKS, true) ||
-      !make(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.codes, 128, chunks, tiles, 512, chunks * 512, 128, St::CHUNKS, per, false) ||
-      !make(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.scales, 8, groups, tiles, 32, groups * 32, 8, St::GROUPS, per, false))
+  if (!make(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT16, p.a, kChunk, p.M, chunks, (cuuint64_t)p.lda * 2, kChunk * 2, kChunk, 8, kStageChunks, true) ||
+      !make(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.codes, 128, chunks, tiles, 512, chunks * 512, 128, kStageChunks, s.wn, false) ||
+      !make(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT32, p.scales, 8, groups, tiles, 32, groups * 32, 8, Stage<G>::GROUPS, s.wn, false))
     return cudaErrorInvalidValue;
-  return launch_pdl(gemm_quantized_stream_kernel<NT, MT, WK, CW, BF, G>, dim3((unsigned)(units < sms ? units : sms)), dim3(32 * (s.wn * WK + 1)), smem, p.st, ta, tc, ts, p.M, p.bias,
-                    p.N, p.K, p.epi, p.out, p.out_bf16, s.wn, s.nst, (uint32_t)stage_bytes_of(MT, WK * CW, G, per), p.status);
+  return launch_pdl(gemm_quantized_stream_kernel<BF, G>, dim3((unsigned)(units < sms ? units : sms)), dim3(32 * (s.wn * WK + 1)), smem, p.st, ta, tc, ts, p.M, p.bias,
+                    p.N, p.K, p.epi, p.out, p.out_bf16, s.wn, s.nst, (uint32_t)stage_bytes_of(G, s.wn), p.status);
 }
 
 template <bool BF, int G>
-cudaError_t launch(const Args& p, const QuantizedGemmShape& s, int mt) {
-  if (!s.stream) {
-    switch (mt) {
-      case 1: return launch_small<1, BF, G>(p, s);
-      case 2: return launch_small<2, BF, G>(p, s);
-      case 3: return launch_small<3, BF, G>(p, s);
-      default: return launch_small<4, BF, G>(p, s);
-    }
+cudaError_t launch(const Args& p, const QuantizedGemmShape& s) {
+  if (s.wn) return launch_stream<BF, G>(p, s);
+  switch ((p.M + 7) / 8) {
+    case 1: return launch_small<1, BF, G>(p, s);
+    case 2: return launch_small<2, BF, G>(p, s);
+    case 3: return launch_small<3, BF, G>(p, s);
+    default: return launch_small<4, BF, G>(p, s);
   }
-  switch (10 * s.nt + mt) {
-    case 11: return launch_stream<1, 1, 4, 2, BF, G>(p, s);
-    case 12: return launch_stream<1, 2, 2, 2, BF, G>(p, s);
-    case 13: return launch_stream<1, 3, 2, 1, BF, G>(p, s);
-    case 23: return launch_stream<2, 3, 2, 1, BF, G>(p, s);
-    case 33: return launch_stream<3, 3, 2, 1, BF, G>(p, s);
-    case 14: return launch_stream<1, 4, 2, 1, BF, G>(p, s);
-    case 24: return launch_stream<2, 4, 2, 1, BF, G>(p, s);
-    case 34: return launch_stream<3, 4, 2, 1, BF, G>(p, s);
-  }
-  return cudaErrorInvalidValue;
 }
 
 }  // namespace
@@ -493,11 +464,11 @@ cudaError_t launch(const Args& p, const QuantizedGemmShape& s, int mt) {
 cudaError_t launch_gemm_quantized(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
                                   int epilogue, void* out, bool a_bf16, int* status, cudaStream_t st) {
   const QuantizedGemmShape s = gemm_quantized_pick(M, N, K, group);
-  const int mt = M > kMaxRows ? kMaxRows / 8 : (M + 7) / 8;
+  if (s.tc) return launch_gemm_quantized_tc(a, lda, M, codes, scales, bias, N, K, group, epilogue, out, a_bf16, s.tc, status, st);
   // (the bias epilogue's output is bf16 in every 16-bit context)
   const Args p = {a, lda, M, codes, scales, bias, N, K, group, epilogue, out, epilogue == 0 || a_bf16, status, st};
-  if (a_bf16) return group == 32 ? launch<true, 32>(p, s, mt) : group == 64 ? launch<true, 64>(p, s, mt) : launch<true, 128>(p, s, mt);
-  return group == 32 ? launch<false, 32>(p, s, mt) : group == 64 ? launch<false, 64>(p, s, mt) : launch<false, 128>(p, s, mt);
+  if (a_bf16) return group == 32 ? launch<true, 32>(p, s) : group == 64 ? launch<true, 64>(p, s) : launch<true, 128>(p, s);
+  return group == 32 ? launch<false, 32>(p, s) : group == 64 ? launch<false, 64>(p, s) : launch<false, 128>(p, s);
 }
 
 cudaError_t launch_quantize_weights(const float* w, int N, int K, int group, void* codes, void* scales, cudaStream_t st) {

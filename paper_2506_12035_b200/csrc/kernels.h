@@ -185,11 +185,16 @@ cudaError_t launch_attention_quantized_tc(const void* q, int ld_q, int n, int he
                                           bool o_bf16, int* status, cudaStream_t st);
 
 // K2 on weights of 4 bits.  N % 16 == 0, K % 64 == 0, group 32, 64 or 128 dividing K; lda % 8 == 0, 16-byte aligned operands.
-struct QuantizedGemmShape { int stream, warps, nt, wn, wk, cw, nst; };
+// How a projection is cut: one of warps (per CTA, small matrices), wn (tiles of a unit, with nst stages; large, up to 8 rows) and tc (CTAs of a
+// cluster; large, more rows) is not 0.
+struct QuantizedGemmShape { int warps, wn, nst, tc; };
 QuantizedGemmShape gemm_quantized_pick(int M, int N, int K, int group);
 size_t gemm_quantized_smem(int M, int group, const QuantizedGemmShape& s);
 cudaError_t launch_gemm_quantized(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
                                   int epilogue, void* out, bool a_bf16, int* status, cudaStream_t st);
+// The same on tcgen05, for large matrices; cs 1, or 2 for pairs of CTAs that split K.
+cudaError_t launch_gemm_quantized_tc(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
+                                     int epilogue, void* out, bool a_bf16, int cs, int* status, cudaStream_t st);
 cudaError_t launch_quantize_weights(const float* w, int N, int K, int group, void* codes, void* scales, cudaStream_t st);
 
 // Diagnostic: one thread waits, with the library's bounded mbarrier wait, on a barrier nothing ever

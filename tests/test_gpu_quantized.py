@@ -436,7 +436,7 @@ def test_linear(models, operand, N, K, group, M):
 
 
 @pytest.mark.parametrize("operand", ["f16", "bf16"])
-@pytest.mark.parametrize("N,K,group", [(4752, 4160, 64), (4768, 4160, 32), (16384, 640, 128), (14240, 704, 32), (9600, 2112, 64)])
+@pytest.mark.parametrize("N,K,group", [(4752, 4160, 64), (4768, 4160, 32), (16384, 640, 128), (14240, 704, 32), (9600, 2112, 64), (18960, 640, 64)])
 @pytest.mark.parametrize("M", [1, 8, 13, 16, 20, 31, 41])
 def test_linear_of_large_matrices(models, operand, N, K, group, M):
     """Matrices that flow through a ring: ragged last units, last stages and last groups of rows."""
@@ -452,6 +452,24 @@ def test_linear_of_large_matrices(models, operand, N, K, group, M):
         m.linear_quantized(a, q, bias, 0, o)
     assert_linear(outs[0], a, codes, scales, group, bias, 0, None)
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("N,K,M", [(768, 256, 2), (4768, 4160, 3), (4768, 4160, 20)])
+def test_weights_laid_out_right_before_the_product(models, N, K, M):
+    """A projection fetches its first codes ahead of what the kernel before it wrote, but not ahead of its own weights' layout."""
+    m, gen = models["bf16"], gen_of(N + M)
+    a, bias = randn(gen, M, K).to(torch.bfloat16), randn(gen, N)
+    ws = [matrix(gen, N, K) * (i + 1) for i in range(4)]
+    want = [torch.empty(M, N, dtype=torch.bfloat16, device="cuda") for _ in ws]
+    for w, o in zip(ws, want):
+        q = m.quantize_weights(w, 64)
+        torch.cuda.synchronize()
+        m.linear_quantized(a, q, bias, 0, o)
+    out = [torch.empty_like(o) for o in want]
+    for _ in range(5):
+        for w, o in zip(ws, out):
+            m.linear_quantized(a, m.quantize_weights(w, 64), bias, 0, o)   # (the matrix before lies in the same memory)
+        assert all(torch.equal(x, y) for x, y in zip(out, want))
 
 
 def test_every_code_and_a_scale_that_is_not_a_number(models):

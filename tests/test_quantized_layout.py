@@ -72,7 +72,7 @@ def test_attention_cuts_fit_an_sm_and_cover_all_rows(lib):
 
 
 class GemmShape(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("stream", "warps", "nt", "wn", "wk", "cw", "nst")]
+    _fields_ = [(n, C.c_int) for n in ("warps", "wn", "nst", "tc")]
 
 
 def test_projection_cuts_fit_an_sm(lib):
@@ -88,15 +88,15 @@ def test_projection_cuts_fit_an_sm(lib):
                         continue
                     s = pick(M, 16 * tiles, 64 * chunks, group)
                     at = (M, tiles, chunks, group, [getattr(s, n) for n, _ in GemmShape._fields_])
-                    mt = min((M + 7) // 8, 4)
-                    if s.stream:
-                        assert (s.nt, mt, s.wk, s.cw) in [(1, 1, 4, 2), (1, 2, 2, 2)] + [(nt, mt, 2, 1) for nt in (1, 2, 3) for mt in (3, 4)], at
-                        assert s.wk * s.wn <= (28 if s.wk == 4 else 14 if s.nt <= 2 else 8) and s.nt * s.wn <= 32 and 3 <= s.nst <= 16, at
-                        assert smem(M, group, C.byref(s)) <= 220 * 1024, at
-                        seen.add((s.nt, mt))
+                    assert (s.warps > 0) + (s.wn > 0) + (s.tc > 0) == 1, at
+                    seen.add((s.warps > 0, s.wn > 0, s.tc))
+                    if s.tc:
+                        assert M > 8 and s.tc in (1, 2) and (s.tc == 1 or chunks > 4), at           # a pair's halves of K are not empty
+                    elif s.wn:
+                        assert M <= 8 and 4 <= s.wn <= 7 and 3 <= s.nst <= 16 and smem(M, group, C.byref(s)) <= 220 * 1024, at
                     else:
-                        assert 1 <= s.warps <= 16 and smem(M, group, C.byref(s)) <= 48 * 1024, at
-    assert len(seen) >= 4
+                        assert s.warps <= 16 and smem(M, group, C.byref(s)) <= 48 * 1024, at
+    assert seen == {(True, False, 0), (False, True, 0), (False, False, 1), (False, False, 2)}
 
 
 @pytest.mark.parametrize("R,S,dh,items,want", [
