@@ -276,20 +276,19 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __gri
             const int e = 2 * parity + (d >> parity & 1);
             if (!__all_sync(0xffffffffu, ptx::mbar_wait(bar(B_D_FULL + e), (uint32_t)(d_phase >> parity) & 1u, abort_flag))) { ok = false; break; }
             ptx::tc_fence_after();
+            uint32_t x[C::DG][NR];
 #pragma unroll
-            for (int i = 0; i < C::DG; ++i) {
-              uint32_t x[NR];
+            for (int i = 0; i < C::DG; ++i)
 #pragma unroll
-              for (int q = 0; q < NR / 16; ++q) tmem_ld_32x16(d_at + (uint32_t)((e * C::DG + i) * NR + 16 * q), x + 16 * q);
-              ptx::tmem_ld_wait();
-              if (i == C::DG - 1) {
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(bar(B_D_EMPTY + e));
-              }
+              for (int q = 0; q < NR; q += 16) tmem_ld_32x16(d_at + (uint32_t)((e * C::DG + i) * NR + q), x[i] + q);
+            ptx::tmem_ld_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(B_D_EMPTY + e));
 #pragma unroll
-              for (int q = 0; q < NR; ++q) acc[q] = fmaf(__uint_as_float(x[q]), scale[i], acc[q]);
-            }
+            for (int i = 0; i < C::DG; ++i)
+#pragma unroll
+              for (int q = 0; q < NR; ++q) acc[q] = fmaf(__uint_as_float(x[i][q]), scale[i], acc[q]);
             d ^= 1 << parity;
             d_phase ^= ~d & (1 << parity);
           }
@@ -327,12 +326,15 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __gri
           const size_t at = (size_t)row0 * sh.N + n;
           if (sh.epi == 1) {                               // (all loads ahead of the stores: one after the other took 16 kcycles a unit)
             float* o = reinterpret_cast<float*>(out) + at;
-            float res[NR];
 #pragma unroll
-            for (int i = 0; i < NR; ++i) res[i] = i >= from && i < rows ? o[(size_t)i * sh.N] : 0.f;
+            for (int q = 0; q < NR; q += 16) {
+              float res[16];
 #pragma unroll
-            for (int i = 0; i < NR; ++i)
-              if (i >= from && i < rows) o[(size_t)i * sh.N] = res[i] + (acc[i] + bn);
+              for (int i = 0; i < 16; ++i) res[i] = q + i >= from && q + i < rows ? o[(size_t)(q + i) * sh.N] : 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (q + i >= from && q + i < rows) o[(size_t)(q + i) * sh.N] = res[i] + (acc[q + i] + bn);
+            }
           } else {
             uint16_t* o = reinterpret_cast<uint16_t*>(out) + at;
 #pragma unroll
