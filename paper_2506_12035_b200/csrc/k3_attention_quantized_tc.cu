@@ -170,7 +170,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
   auto bar = [&](int j, int i) { return base + C::OFF_BAR + 8u * (uint32_t)(j * NB + i); };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + C::OFF_MISC + 8);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int units_cta = deal.units / deal.grid + (deal.place<NS>(deal.units / deal.grid) < deal.units % deal.grid ? 1 : 0);
 
   if (threadIdx.x == 0) {
@@ -195,8 +195,10 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
   pdl_sync();
 
   if (warp >= C::W_MMA) {
-    // ---------------------------------------------------------------- MMA issuer of stream j
-    if (ptx::elect_one()) {
+    // ---------------------------------------------------------------- MMA issuer of stream j.  The whole warp runs the loop and one lane issues, so that
+    // descriptors can stay in uniform registers (in a branch of one lane an MMA takes 70 cycles to issue, more than to run)
+    {
+      const bool issuer = ptx::elect_one();
       const int j = warp - C::W_MMA, n_units = (units_cta + NS - 1 - j) / NS;
       constexpr uint32_t idesc_s = idesc_f16(QT, KT, false), idesc_o = idesc_f16(QT, 64, true), idesc_tail = idesc_f16(QT, 16, true);
       const uint32_t d_s = tmem_base + (uint32_t)j * C::COL_STREAM, d_p = d_s + C::COL_P, d_o = d_s + C::COL_O;
@@ -214,12 +216,13 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
       int s_slot = 0, o_slot = 0;
       uint32_t k_phase = 0, v_phase = 0, q_phase = 0;
       bool ok = true;
+      auto wait = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar(j, i), parity, abort_flag)) != 0; };
       auto wait_s = [&]() -> bool {
         if (ws.i == 0) {
-          if (!ptx::mbar_wait(bar(j, B_Q_FULL), q_phase, abort_flag)) return false;
+          if (!wait(B_Q_FULL, q_phase)) return false;
           q_phase ^= 1u;
         }
-        return ptx::mbar_wait(bar(j, B_K_FULL + s_slot), k_phase, abort_flag);
+        return wait(B_K_FULL + s_slot, k_phase);
       };
       auto issue_s = [&]() {
         const uint32_t kt = k0 + (uint32_t)s_slot * C::T_BYTES;
@@ -227,12 +230,16 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         for (int bl = 0; bl < C::BLOCKS; ++bl) {
           const uint64_t dq = ptx::smem_desc_k_sw128(q0 + bl * C::Q_BLOCK), dk = ptx::smem_desc_k_sw128(kt + bl * C::T_BLOCK);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) ptx::umma_f16(d_s, dq + 2 * k, dk + 2 * k, idesc_s, (bl | k) ? 1u : 0u);
+          for (int k = 0; k < 4; ++k)
+            if (issuer) ptx::umma_f16(d_s, dq + 2 * k, dk + 2 * k, idesc_s, (bl | k) ? 1u : 0u);
         }
-        if (C::TAIL) ptx::umma_f16(d_s, smem_desc_sw32(q0 + C::BLOCKS * C::Q_BLOCK), smem_desc_sw32(kt + C::BLOCKS * C::T_BLOCK), idesc_s, 1u);
-        ptx::umma_commit(bar(j, B_S_FULL));
-        ptx::umma_commit(bar(j, B_K_EMPTY + s_slot));
-        if (ws.i + 1 == ws.n) ptx::umma_commit(bar(j, B_Q_EMPTY));       // the unit's last: its rows may be overwritten
+        if (C::TAIL && issuer) ptx::umma_f16(d_s, smem_desc_sw32(q0 + C::BLOCKS * C::Q_BLOCK), smem_desc_sw32(kt + C::BLOCKS * C::T_BLOCK), idesc_s, 1u);
+        if (issuer) {
+          ptx::umma_commit(bar(j, B_S_FULL));
+          ptx::umma_commit(bar(j, B_K_EMPTY + s_slot));
+          if (ws.i + 1 == ws.n) ptx::umma_commit(bar(j, B_Q_EMPTY));     // the unit's last: its rows may be overwritten
+        }
+        __syncwarp();
         if (++s_slot == NB2) { s_slot = 0; k_phase ^= 1u; }
       };
       bool more_s = next_unit(ws), more_o = next_unit(wo);
@@ -244,28 +251,31 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
       for (int t = 0; more_o && ok; ++t) {
         if (more_s && ++ws.i == ws.n) more_s = next_unit(ws);
         if (more_s) {                                      // the logits are in registers: the next ones may come
-          if (!wait_s() || !ptx::mbar_wait(bar(j, B_S_FREE), (uint32_t)t & 1u, abort_flag)) { ok = false; break; }
+          if (!wait_s() || !wait(B_S_FREE, (uint32_t)t & 1u)) { ok = false; break; }
           ptx::tc_fence_after();
           issue_s();
         }
-        if (!ptx::mbar_wait(bar(j, B_V_FULL + o_slot), v_phase, abort_flag) ||
+        if (!wait(B_V_FULL + o_slot, v_phase) ||
             // (for a unit's first tile the previous output has been read out: every softmax warp did so before it wrote)
-            !ptx::mbar_wait(bar(j, B_P_FULL), (uint32_t)t & 1u, abort_flag)) { ok = false; break; }
+            !wait(B_P_FULL, (uint32_t)t & 1u)) { ok = false; break; }
         ptx::tc_fence_after();
         const uint32_t vt = v0 + (uint32_t)o_slot * C::T_BYTES;
 #pragma unroll
         for (int k = 0; k < KT / 16; ++k) {
 #pragma unroll
           for (int bl = 0; bl < C::BLOCKS; ++bl)
-            umma_f16_ts(d_o + 64u * bl, d_p + 8u * k, smem_desc_mn_sw128(vt + bl * C::T_BLOCK) + 128 * k, idesc_o, (wo.i | k) ? 1u : 0u);
-          if (C::TAIL) umma_f16_ts(d_o + 64u * C::BLOCKS, d_p + 8u * k, smem_desc_sw32(vt + C::BLOCKS * C::T_BLOCK) + 32 * k, idesc_tail, (wo.i | k) ? 1u : 0u);
+            if (issuer) umma_f16_ts(d_o + 64u * bl, d_p + 8u * k, smem_desc_mn_sw128(vt + bl * C::T_BLOCK) + 128 * k, idesc_o, (wo.i | k) ? 1u : 0u);
+          if (C::TAIL && issuer) umma_f16_ts(d_o + 64u * C::BLOCKS, d_p + 8u * k, smem_desc_sw32(vt + C::BLOCKS * C::T_BLOCK) + 32 * k, idesc_tail, (wo.i | k) ? 1u : 0u);
         }
-        ptx::umma_commit(bar(j, B_O_FULL));
-        ptx::umma_commit(bar(j, B_V_EMPTY + o_slot));
+        if (issuer) {
+          ptx::umma_commit(bar(j, B_O_FULL));
+          ptx::umma_commit(bar(j, B_V_EMPTY + o_slot));
+        }
+        __syncwarp();
         if (++o_slot == NB2) { o_slot = 0; v_phase ^= 1u; }
         if (++wo.i == wo.n) more_o = next_unit(wo);
       }
-      if (!ok) *(volatile int*)status = ST_ATT_QUANTIZED_TC;
+      if (!ok && issuer) *(volatile int*)status = ST_ATT_QUANTIZED_TC;
     }
   } else if (warp >= C::W_PROD) {
     // ---------------------------------------------------------------- TMA producer of stream j
