@@ -503,14 +503,14 @@ size_t marche_quantized_weights_bytes(int n, int k, int group, size_t* scales_by
 
 /* Lays out w, device float [n][k] dense, in out->codes and out->scales: scale = max |w| / 7 of the group rounded
  * to bf16, code = w / scale rounded to nearest, ties to even, and clamped to -7 .. 7; a group that holds an infinity
- * or a NaN gets a NaN scale.  Asynchronous. */
+ * or a NaN gets a NaN scale.  Asynchronous; marche_linear_quantized may follow in the same stream. */
 int marche_quantize_weights(marche_ctx* ctx, const float* w, const marche_quantized_weights* out, marche_stream stream);
 
 /* out = epilogue(a * w^T + bias) with the epilogues and element types of marche_linear; a is A [M][k] with row
  * stride lda (lda % 8 == 0).  Meant for few rows: 32 share a pass over the matrix, more repeat it; M up to
  * MARCHE_QUANTIZED_MAX_ROWS (MARCHE_ESHAPE).  fp32 accumulation of exact products; GELU with the exact erf.  The weights
- * are fetched before the preceding kernel of the stream has finished: they must be complete in memory, as for
- * marche_linear (synchronise after laying them out, or keep another kernel of the stream in between). */
+ * are fetched before the preceding kernel of the stream has finished: unless marche_quantize_weights wrote them, they must
+ * be complete in memory, as for marche_linear (synchronise, or keep another kernel of the stream in between). */
 #define MARCHE_QUANTIZED_MAX_ROWS 65536
 int marche_linear_quantized(marche_ctx* ctx, const void* a, int lda, int M, const marche_quantized_weights* w,
                             const float* bias, int epilogue, void* out, marche_stream stream);

@@ -11,6 +11,9 @@
 // 1024 + 16 c for the nibble above it; one packed subtraction or FMA takes 1032 (or 64 + 8 after the division by 16) off, exactly.
 // Products of a group add up in fp32 in the tensor core, are scaled once per group and output in fp32 and added in fp32; the warps of a
 // CTA take the inputs in turn and their sums meet in shared memory in a fixed order (bit-reproducible).  No other rounding before the last.
+// Three kernels: this file's two, for small matrices and for up to eight rows of large ones, and k2_gemm_quantized_tc.cu for more rows.  With
+// 9 to 32 rows of a large matrix the work of a warp here (90 to 110 instructions for 16 outputs x 64 inputs x 32 rows: operands, conversion, sums of a
+// group, barriers) exceeded the bytes' time four times: 31 x 24576 x 12288 97 us.
 #include "common.cuh"
 #include "kernels.h"
 #include "launch_pdl.h"

@@ -2,13 +2,16 @@
 //
 // out^T = w a^T: 128 outputs are the rows of the A operand, which tcgen05.mma reads from tensor memory, 16 or 32 rows of a the columns of B (shared
 // memory, as TMA brings them).  A thread owns an output: it takes the output's 64 codes of a chunk (32 bytes) from shared memory, makes fp16
-// (bf16) numbers of them (exact, see k2_gemm_quantized.cu), and stores them to its tensor-memory lane: no fragment is converted twice, and what
-// the mma.sync kernel spends on operand loads, partial sums and barriers (90 to 110 instructions for 16 outputs x 64 inputs) is gone.
-// Sums of a group (32, 64 or 128 inputs) accumulate in tensor memory in fp32; four other warps, a thread per output again, read them, multiply by
-// the group's scale and add them up in fp32 registers, which are stored as whole lines at the end.
+// (bf16) numbers of them (exact, see k2_gemm_quantized.cu), and stores them to its tensor-memory lane.  Sums of a group (32, 64 or 128 inputs)
+// accumulate in tensor memory in fp32; four other warps, a thread per output again, read them, multiply by the group's scale and add them up in
+// fp32 registers, which are stored as whole lines at the end.
 // Persistent CTAs, one per SM, or pairs (a cluster) that split K where that divides the units more evenly: the halves' sums meet by st.async in the
-// CTA that owns the row.  Warps: 0-3 and 4-7 convert the even and odd chunks (two A buffers each), 8-11 add up, 12 fetches, 13 issues MMAs.
-// What bounds it: HBM; then the conversion, 96 integer and packed-fp16 instructions of a warp for 32 outputs x 64 inputs.  All waits are bounded.
+// CTA that owns the row (31 x 24576 x 12288, 192 units: 61 and 52 us).  Stages of 256 inputs; warps: 0-3 convert the even stages, 4-7 the odd ones, 8-11 add
+// up, 12 fetches, 13 and 14 issue MMAs of even and odd stages.  All waits are bounded and report through the status word.
+// What bounds it: the conversion's instructions (per 64 inputs of 32 outputs 48 integer ones at two cycles each and 32 packed FMAs), 1200 cycles a stage
+// where its bytes would take 700; half of the issue slots, 40 % of the integer pipe, and 72 stages on the busiest SM for 62 on average.
+// 31 x 24576 x 12288, group 128: 52 us of 25 for the bytes (3.0 TB/s); group 64 59 us, group 32 79 us (sums twice and four times as often).
+// On the way: stages of 128 inputs 104 us; residual rows loaded one after the other in the epilogue 80; one MMA warp, one lane's branch 55.
 #include <cuda.h>
 
 #include "kernels.h"

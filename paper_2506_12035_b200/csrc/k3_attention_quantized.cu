@@ -6,6 +6,8 @@
 // is rounded is the weight: p vs / 2^e to fp16 (11 bits), where 2^e bounds the largest value scale met so far and the whole is
 // lifted by 2^14, so that a weight 2^-28 of the largest possible keeps all its bits.  Maxima, sums and accumulators are fp32, and the running
 // exponent e moves with the running maximum (one factor for both).
+// Where the output is fp16, what that rounding left off follows as a second operand (FINE): with one rounding of as many bits as the output's own the
+// error is 1.4 times the output's, 1.55 over few keys.  A bf16 output, eight times coarser, does not need it.
 // Query heads that share a cached head are rows of one item: row r is token r / G, head r % G of the group.
 //
 // mma.sync m16n8k16 on the transposed products, S^T = K q^T and O^T = V^T P^T: keys (then columns of V) are the 16-row operand and the
@@ -123,7 +125,7 @@ MARCHE_DEVINL void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint
 MARCHE_DEVINL float pow2(int biased_exponent) { return __int_as_float(biased_exponent << 23); }
 
 // Grid: B * H * n_rb * cs CTAs, the cs of a cluster next to one another.
-template <int DH, int NB>
+template <int DH, int NB, bool FINE>
 __global__ void __launch_bounds__(kThreadsMax)
 attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16* __restrict__ q, int ld_q, int n, int heads, int H, int G, int B, int S,
                            int pad, const float* __restrict__ scales, const int32_t* __restrict__ kv_len, uint16_t* __restrict__ o, int o_bf16,
@@ -345,7 +347,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
       for (int m = 0; m < NB; ++m) ls[m][0] = ls[m][1] = 0.f;
 #pragma unroll
       for (int i = 0; i < NM; ++i) {
-        uint32_t pb[NB][2];
+        uint32_t pb[NB][2], pl[NB][2];
         float f0 = vs[16 * i + g], f1 = vs[16 * i + g + 8];
         mul2(f0, f1, lift, lift);
 #pragma unroll
@@ -358,7 +360,12 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
             p1 = ex2_approx(p1);
             add2(ls[m][0], ls[m][1], p0, p1);
             mul2(p0, p1, hf ? f1 : f0, hf ? f1 : f0);
-            pb[m][hf] = turn8x8(pack_weights(p0, p1));
+            const uint32_t w = pack_weights(p0, p1);
+            pb[m][hf] = turn8x8(w);
+            if (FINE) {
+              const float2 hi = unpack_f16x2(w);
+              pl[m][hf] = turn8x8(pack_weights(p0 - hi.x, p1 - hi.y));
+            }
           }
         const int key = 16 * i + 8 * ((lane >> 3) & 1) + (lane & 7);
 #pragma unroll
@@ -371,7 +378,10 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
             const uint32_t lo = w[2 * d] ^ 0x80808080u, hi = w[2 * d + 1] ^ 0x80808080u;
             const uint32_t a[4] = {two_of<0x4240>(lo), two_of<0x4341>(lo), two_of<0x4240>(hi), two_of<0x4341>(hi)};
 #pragma unroll
-            for (int m = 0; m < NB; ++m) mma_f16(oacc[m][c + d], a, pb[m][0], pb[m][1]);
+            for (int m = 0; m < NB; ++m) {
+              mma_f16(oacc[m][c + d], a, pb[m][0], pb[m][1]);
+              if (FINE) mma_f16(oacc[m][c + d], a, pl[m][0], pl[m][1]);
+            }
           }
         }
       }
@@ -487,7 +497,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
   }
 }
 
-template <int DH, int NB>
+template <int DH, int NB, bool FINE>
 cudaError_t launch(const void* q, int ld_q, int n, int heads, const QuantizedKv& c, const int32_t* kv_len, void* o, bool o_bf16, const QuantizedSplit& s,
                    int* status, cudaStream_t st) {
   using C = Cfg<DH, NB>;
@@ -502,10 +512,10 @@ cudaError_t launch(const void* q, int ld_q, int n, int heads, const QuantizedKv&
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
-  cudaError_t e = ensure_dynamic_smem(attention_quantized_kernel<DH, NB>, smem, smem_set);
+  cudaError_t e = ensure_dynamic_smem(attention_quantized_kernel<DH, NB, FINE>, smem, smem_set);
   if (e != cudaSuccess) return e;
   const int G = heads / c.H;
-  return launch_pdl_cluster(attention_quantized_kernel<DH, NB>, dim3((unsigned)((long)c.B * c.H * s.n_rb * s.cs)), dim3(s.nr * s.nk * 32), smem, s.cs, st, tm,
+  return launch_pdl_cluster(attention_quantized_kernel<DH, NB, FINE>, dim3((unsigned)((long)c.B * c.H * s.n_rb * s.cs)), dim3(s.nr * s.nk * 32), smem, s.cs, st, tm,
                             (const bf16*)q, ld_q, n, heads, c.H, G, c.B, c.S, c.pad, (const float*)c.scales, kv_len, (uint16_t*)o, o_bf16 ? 1 : 0, s, status);
 }
 
@@ -559,7 +569,8 @@ cudaError_t launch_attention_quantized(const void* q, int ld_q, int n, int heads
                                        int* status, cudaStream_t st) {
   const QuantizedSplit s = attention_quantized_plan(n * (heads / c.H), c.S, c.dh, c.B * c.H);
 #define MARCHE_QA(DH_, NB_) \
-  case DH_ * 8 + NB_: return launch<DH_, NB_>(q, ld_q, n, heads, c, kv_len, o, o_bf16, s, status, st);
+  case DH_ * 8 + NB_:                                      \
+    return o_bf16 ? launch<DH_, NB_, false>(q, ld_q, n, heads, c, kv_len, o, true, s, status, st) : launch<DH_, NB_, true>(q, ld_q, n, heads, c, kv_len, o, false, s, status, st);
   switch (c.dh * 8 + s.nb) {
     MARCHE_QA(64, 1) MARCHE_QA(64, 2) MARCHE_QA(80, 1) MARCHE_QA(80, 2) MARCHE_QA(128, 1) MARCHE_QA(128, 2)
   }

@@ -468,7 +468,8 @@ def test_weights_laid_out_right_before_the_product(models, N, K, M):
     out = [torch.empty_like(o) for o in want]
     for _ in range(5):
         for w, o in zip(ws, out):
-            m.linear_quantized(a, m.quantize_weights(w, 64), bias, 0, o)   # (the matrix before lies in the same memory)
+            assert m.lib.marche_quantize_weights(m.h, w.data_ptr(), q.ref, torch.cuda.current_stream().cuda_stream) == 0   # (without the binding's wait)
+            m.linear_quantized(a, q, bias, 0, o)
         assert all(torch.equal(x, y) for x, y in zip(out, want))
 
 
