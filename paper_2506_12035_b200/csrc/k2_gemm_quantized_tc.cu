@@ -42,10 +42,6 @@ template <int NR, int G> struct Cfg {
   static constexpr uint32_t COL_A = 0, COL_D = 2 * SC * 32, COLS = 512;   // A: two buffers of SC chunks, 32 columns each; D: four of DG groups of NR
 };
 
-MARCHE_DEVINL void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst), "l"(map), "r"(bar), "r"(c0),
-               "r"(c1), "r"(c2), "r"(c3) : "memory");
-}
 MARCHE_DEVINL void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n"
@@ -137,7 +133,7 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __gri
       auto load_codes = [&](int slot, int tile0, int s) {
         const uint32_t dst = ring + (uint32_t)(slot * C::STAGE), b = bar(B_FULL + slot);
         ptx::mbar_expect_tx(b, C::FILL);
-        tma_load_4d(dst + C::ROWS, &tmap_codes, 0, 0, s * SC, tile0, b);
+        ptx::tma_load_4d(dst + C::ROWS, &tmap_codes, 0, 0, s * SC, tile0, b);
         ptx::tma_load_3d(dst + C::ROWS + C::CODES, &tmap_scales, 0, s * C::GROUPS, tile0, b);
       };
       auto load_rows = [&](int slot, int row0, int s) { ptx::tma_load_3d(ring + (uint32_t)(slot * C::STAGE), &tmap_a, 0, row0, s * SC, bar(B_FULL + slot)); };

@@ -119,16 +119,13 @@ MARCHE_DEVINL uint32_t turn8x8(uint32_t x) {               // an 8 x 8 matrix of
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-MARCHE_DEVINL void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
 MARCHE_DEVINL float pow2(int biased_exponent) { return __int_as_float(biased_exponent << 23); }
 
 // Grid: B * H * n_rb * cs CTAs, the cs of a cluster next to one another.
 template <int DH, int NB, bool FINE>
 __global__ void __launch_bounds__(kThreadsMax)
-attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16* __restrict__ q, int ld_q, int n, int heads, int H, int G, int B, int S,
-                           int pad, const float* __restrict__ scales, const int32_t* __restrict__ kv_len, uint16_t* __restrict__ o, int o_bf16,
+attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_scales, const bf16* __restrict__ q, int ld_q, int n, int heads, int H, int G, int B, int S,
+                           const int32_t* __restrict__ kv_len, uint16_t* __restrict__ o, int o_bf16,
                            const QuantizedSplit sp, int* __restrict__ status) {
   using C = Cfg<DH, NB>;
   constexpr int RPW = 8 * NB, KT = C::KT, NM = C::NM;      // rows of a warp
@@ -156,6 +153,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
     ptx::prefetch_tensormap(&tmap);
+    ptx::prefetch_tensormap(&tmap_scales);
   }
   __syncwarp();
   if (sp.cs > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -167,16 +165,15 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const bf16*
   const int tiles = (len + KT - 1) / KT;
   const int kt0 = (int)((long long)rank * tiles / sp.cs), n_tiles = (int)((long long)(rank + 1) * tiles / sp.cs) - kt0;
   const int mine = (n_tiles - wk + sp.nk - 1) / sp.nk, stage0 = wk * sp.nst;   // tiles wk, wk + nk, .. of the CTA's; the group's first stage
-  // The group's next tile into its next stage (lane 0 of its first warp).
+  // The group's next tile into its next stage (lane 0 of its first warp): K and V by one copy, both scales by another (four copies took 88 -> 94 us
+  // for 4 x 65521 keys; a warp of its own for the refills costs registers, that is CTAs on an SM, and ties the groups to one another: 112).
   int f_slot = 0, issued = 0;
   auto load = [&]() {
     const int s = stage0 + f_slot, kt = kt0 + wk + issued * sp.nk;
     const uint32_t bar = full0 + 8u * s, dst = base + (uint32_t)(s * C::STAGE), dst_s = scale_base + (uint32_t)(s * C::SCALES);
     ptx::mbar_expect_tx(bar, C::STAGE + C::SCALES);
-    ptx::tma_load_3d(dst, &tmap, h * DH, kt * KT, b, bar);
-    ptx::tma_load_3d(dst + C::TILE, &tmap, h * DH, kt * KT, B + b, bar);
-    bulk_load(dst_s, scales + ((size_t)b * H + h) * pad + (size_t)kt * KT, KT * 4, bar);
-    bulk_load(dst_s + KT * 4, scales + ((size_t)(B + b) * H + h) * pad + (size_t)kt * KT, KT * 4, bar);
+    ptx::tma_load_4d(dst, &tmap, h * DH, kt * KT, b, 0, bar);
+    ptx::tma_load_3d(dst_s, &tmap_scales, kt * KT, b * H + h, 0, bar);
     ++issued;
     if (++f_slot == sp.nst) f_slot = 0;
   };
@@ -503,20 +500,24 @@ cudaError_t launch(const void* q, int ld_q, int n, int heads, const QuantizedKv&
   using C = Cfg<DH, NB>;
   const size_t smem = attention_quantized_smem(DH, s);
   if (smem > 226 * 1024) return cudaErrorInvalidValue;
-  CUtensorMap tm;
+  // boxes of a tile: K and V [2][keys][dh], their scales [2][keys]
+  CUtensorMap tm, ts;
   EncodeTiledFn fn = tma_encode_fn();
-  const cuuint64_t D = (cuuint64_t)c.H * DH, dims[3] = {D, (cuuint64_t)c.S, (cuuint64_t)2 * c.B}, strides[2] = {D, D * c.S};
-  const cuuint32_t box[3] = {DH, C::KT, 1}, unit[3] = {1, 1, 1};
+  const cuuint64_t D = (cuuint64_t)c.H * DH, dims[4] = {D, (cuuint64_t)c.S, (cuuint64_t)c.B, 2}, strides[3] = {D, D * c.S, D * c.S * c.B};
+  const cuuint64_t dims_s[3] = {(cuuint64_t)c.pad, (cuuint64_t)c.B * c.H, 2}, strides_s[2] = {(cuuint64_t)c.pad * 4, (cuuint64_t)c.pad * 4 * c.B * c.H};
+  const cuuint32_t box[4] = {DH, C::KT, 1, 2}, box_s[3] = {C::KT, 1, 2}, unit[4] = {1, 1, 1, 1};
   const CUtensorMapSwizzle sw = DH == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : DH == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
-  if (!fn || fn(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, c.codes, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  if (!fn || fn(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, c.codes, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+      fn(&ts, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, c.scales, dims_s, strides_s, box_s, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
   cudaError_t e = ensure_dynamic_smem(attention_quantized_kernel<DH, NB, FINE>, smem, smem_set);
   if (e != cudaSuccess) return e;
   const int G = heads / c.H;
-  return launch_pdl_cluster(attention_quantized_kernel<DH, NB, FINE>, dim3((unsigned)((long)c.B * c.H * s.n_rb * s.cs)), dim3(s.nr * s.nk * 32), smem, s.cs, st, tm,
-                            (const bf16*)q, ld_q, n, heads, c.H, G, c.B, c.S, c.pad, (const float*)c.scales, kv_len, (uint16_t*)o, o_bf16 ? 1 : 0, s, status);
+  return launch_pdl_cluster(attention_quantized_kernel<DH, NB, FINE>, dim3((unsigned)((long)c.B * c.H * s.n_rb * s.cs)), dim3(s.nr * s.nk * 32), smem, s.cs, st, tm, ts,
+                            (const bf16*)q, ld_q, n, heads, c.H, G, c.B, c.S, kv_len, (uint16_t*)o, o_bf16 ? 1 : 0, s, status);
 }
 
 }  // namespace

@@ -108,6 +108,12 @@ MARCHE_DEVINL void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int
       ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
+MARCHE_DEVINL void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
 // The same load with an L2 eviction-priority hint: data that is streamed once (the K/V cache during
 // attention) is marked evict-first so that it does not push the step's activations out of L2.
 MARCHE_DEVINL uint64_t l2_policy_evict_first() {
