@@ -496,6 +496,77 @@ def test_every_code_and_a_scale_that_is_not_a_number(models):
         assert s.isnan().sum() == 2 and bool(s[2, 0].isnan()) and bool(s[4, 1].isnan())
 
 
+@pytest.mark.parametrize("operand", ["f16", "bf16"])
+@pytest.mark.parametrize("M", [5, 12, 20])
+def test_every_code_of_a_large_matrix(models, operand, M):
+    """The kernels for large matrices on codes -8 .. 7, a NaN scale, which reaches its output only, and an infinite value, which reaches its row only."""
+    m, gen, N, K = models[operand], gen_of(M), 4768, 4160
+    q = m.quantize_weights(matrix(gen, N, K), 32)
+    q.codes.copy_(torch.randint(0, 256, q.codes.shape, generator=gen, device="cuda").to(torch.uint8))
+    q.scales.copy_(torch.rand(q.scales.shape, generator=gen, device="cuda") + 0.5)
+    codes, scales = unpack(q)
+    assert int(codes.min()) == -8 and int(codes.max()) == 7
+    a, bias, out = randn(gen, M, K).to(TYPES[operand]), randn(gen, N), torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    m.linear_quantized(a, q, bias, 0, out)
+    assert_linear(out, a, codes, scales, 32, bias, 0, None)
+    q.scales[10] = float("nan")                                      # tile 0, group 0, output 5
+    codes[:, 7] = 1
+    q2 = a.clone()
+    q2[3, 7] = float("inf")
+    torch.cuda.synchronize()
+    other = torch.empty_like(out)
+    m.linear_quantized(q2, q, bias, 0, other)
+    keep = torch.ones_like(out, dtype=torch.bool)
+    keep[3], keep[:, 5] = False, False
+    assert bool(other[:, 5].isnan().all()) and not bool(other[3].isfinite().all()) and torch.equal(other[keep], out[keep])
+
+
+@pytest.mark.parametrize("M", [2, 12, 31])
+def test_projections_on_two_streams_and_in_graphs(models, M):
+    """Small and large matrices beside the attention with many rows: on two streams at once, captured on both, replayed over new inputs at once."""
+    m, gen = models["f16"], gen_of(M)
+    shapes = [(768, 256, 64), (4768, 4160, 64), (9600, 2112, 32)]
+    ws = [m.quantize_weights(matrix(gen, N, K), g) for N, K, g in shapes]
+    bias = [randn(gen, w.N) for w in ws]
+    cache = filled_cache(m, gen, 20, 320, 8, 64)
+    rows = [[randn(gen, M, w.K).to(torch.float16) for w in ws] for _ in range(2)]
+    q = randn(gen, 20 * 70, 8 * 64).to(torch.bfloat16)
+
+    def all_of(side, out, o):
+        for a, w, b, y in zip(rows[side], ws, bias, out):
+            m.linear_quantized(a, w, b, 0, y)
+            m.attention_quantized(q, 512, 70, 8, cache, None, o)
+            m.linear_quantized(a, w, b, 0, y)
+    new = lambda: ([torch.empty(M, w.N, dtype=torch.bfloat16, device="cuda") for w in ws], torch.empty(20 * 70, 512, dtype=torch.float16, device="cuda"))
+    want, got, sides = [new(), new()], [new(), new()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k in range(2):
+        all_of(k, *want[k])
+    torch.cuda.synchronize()
+    same = lambda: all(torch.equal(x, y) for k in range(2) for x, y in zip(want[k][0] + [want[k][1]], got[k][0] + [got[k][1]]))
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for _ in range(3):
+        for k in range(2):
+            with torch.cuda.stream(sides[k]):
+                all_of(k, *got[k])
+    torch.cuda.synchronize()
+    assert same()
+    for k in range(2):
+        with torch.cuda.graph(graphs[k], stream=sides[k]):
+            all_of(k, *got[k])
+    for r in rows[0] + rows[1]:
+        r.neg_()
+    for k in range(2):
+        all_of(k, *want[k])
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for k in range(2):
+            with torch.cuda.stream(sides[k]):
+                graphs[k].replay()
+    torch.cuda.synchronize()
+    assert same()
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("operand", ["f16", "bf16"])
 @pytest.mark.parametrize("B,S,n", [(2, 333, 1), (2, 320, 13), (10, 100, 20)])
