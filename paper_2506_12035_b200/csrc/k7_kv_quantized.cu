@@ -1,12 +1,12 @@
 // K7: rows of K and V into a cache held in 8 bits, and rows of that cache back.
 //
 // A head's dh values of one token share a scale: amax = max |x|, code = round(127 x / amax) (ties to even), scale = amax / 127,
-// value = code * scale.  Codes are those of exact arithmetic: 127 x is exact in fp32 for a bf16 x (8 + 7 bits), and the quotient comes from an
-// approximate reciprocal of amax (one per head) with one correction by the remainder 127 x - t amax (Markstein's), which is exact, so
-// that an error of 2^-44 t is left before the last rounding.  A quotient that is not a half is at least 2^-17 away from one (numerator and
-// denominator have few bits), so it rounds to its own side; one that is a half (x = amax / 2 is: 63.5) is a fp32 number, and the correction lands on
-// it.  Rounding is the addition of 1.5 * 2^23, whose sum's low byte is the code.  scale comes by the same correction: a quotient of 8 bits by
-// 127 is at least 2^-32 of itself away from the middle of two fp32 numbers.
+// value = code * scale.  Codes are those of exact arithmetic.  127 / amax is found once per head as the sum of two fp32 numbers, an approximate
+// reciprocal's 127 fold and, of the remainder, which is exact (amax has 8 bits, so it has few), the rest: right to 2^-44.  x times the sum by a
+// product and an FMA is the quotient rounded once, by at most 2^-18 (it is below 128).  A quotient that is not a half is at least 2^-17 away from one
+// (numerator and denominator have few bits), so it stays on its own side; one that is a half (x = amax / 2 is: 63.5) is a fp32 number, and the FMA
+// lands on it.  Rounding is the addition of 1.5 * 2^23, whose sum's low byte is the code.  scale comes from amax / 127 by a multiplication and a
+// correction by the remainder: a quotient of 8 bits by 127 is at least 2^-32 of itself away from the middle of two fp32 numbers.
 // amax comes from the magnitudes, with NaN above infinity above every number: a head that holds one gets codes 0 and a NaN scale, so all of it
 // reads back as NaN, and no code is ever anything but a number.
 //
@@ -14,7 +14,8 @@
 // per lane), all loads of up to four heads a group ahead; the row leaves as whole 32-byte sectors; the scales lie key by key (their readers'
 // order) and leave as single words.  Rows whose token is outside the cache are skipped: a batch with different numbers of rows is padded with -1.
 // 6 x 8191 rows of 16 heads of 64: a division per value and index divisions per head 116 us for the writing (85 % of the issue slots), as it
-// stands 69 us; reading back 53 us, 5.8 TB/s.
+// stands 65 us (a remainder per quotient 69; more registers than five CTAs on an SM have, at head_dim 80 1 us more for 128 x 43 rows); reading back
+// 53 us, 5.8 TB/s.
 #include "common.cuh"
 #include "kernels.h"
 #include "launch_pdl.h"
@@ -52,7 +53,7 @@ MARCHE_DEVINL uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // NaN wins
 
 // blockIdx.y: K or V.  A warp takes a row, U rounds of 32 / W heads at a time.
 template <int DH, int U>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 5)
 scatter_kv_quantized_kernel(const bf16* __restrict__ k, const bf16* __restrict__ v, size_t ld, const int32_t* __restrict__ idx, int n, int rows, int B,
                             int S, int H, int pad, int8_t* __restrict__ codes, float* __restrict__ scales) {
   constexpr int W = DH / 8, HPW = 32 / W;
@@ -82,15 +83,20 @@ scatter_kv_quantized_kernel(const bf16* __restrict__ k, const bf16* __restrict__
       // Both sides of the division move to the range's middle by the same power of two near its ends; a head of zeros, or one that is not
       // finite, is divided by 1.
       const bool plain = top != 0 && top < 0x7f80u;
-      const float amax = __uint_as_float(top << 16), shift = top >= 0x6000u ? 0x1p-64f : (top < 0x2000u ? 0x1p64f : 1.0f);
-      const float d = plain ? amax * shift : 1.0f, inv = rcp_approx(d), times = plain ? 127.0f * shift : 0.f;
+      const float amax = __uint_as_float(top << 16), shift = !plain ? 1.0f : (top >= 0x6000u ? 0x1p-64f : (top < 0x2000u ? 0x1p64f : 1.0f));
+      const float d = plain ? amax * shift : 1.0f, inv = rcp_approx(d), r_hi = 127.0f * inv, r_lo = fmaf(-r_hi, d, 127.0f) * inv;
       if (!plain) words[0] = words[1] = words[2] = words[3] = 0;
+      if (shift != 1.0f) {                                 // (what gets too small for a bf16 here has code 0)
+        const uint32_t both_shifts = __float_as_uint(shift) | (__float_as_uint(shift) >> 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(words[i]) : "r"(both_shifts));
+      }
       uint32_t c[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 n127 = __fmul2_rn(make_float2(__uint_as_float(words[i] << 16), __uint_as_float(words[i] & 0xffff0000u)), make_float2(times, times));
-        const float2 q = __fmul2_rn(n127, make_float2(inv, inv)), rest = __ffma2_rn(make_float2(-q.x, -q.y), make_float2(d, d), n127);
-        const float2 r = __fadd2_rn(__ffma2_rn(rest, make_float2(inv, inv), q), make_float2(12582912.0f, 12582912.0f));
+        const float2 v = make_float2(__uint_as_float(words[i] << 16), __uint_as_float(words[i] & 0xffff0000u));
+        const float2 q = __ffma2_rn(v, make_float2(r_hi, r_hi), __fmul2_rn(v, make_float2(r_lo, r_lo)));
+        const float2 r = __fadd2_rn(q, make_float2(12582912.0f, 12582912.0f));
         c[2 * i] = __float_as_uint(r.x);
         c[2 * i + 1] = __float_as_uint(r.y);
       }
