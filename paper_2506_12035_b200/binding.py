@@ -480,11 +480,13 @@ class Marche:
         return q
 
     def linear_quantized(self, a, w: QuantizedWeights, bias, epilogue, out, M=None, lda=None, stream=None):
-        M = a.shape[0] if M is None else M
-        lda = a.stride(0) if lda is None else lda
         assert a.is_cuda and a.dtype == self.operand_dtype and bias.dtype == torch.float32 and bias.numel() >= w.N
-        if M > 0 and not (a.stride() == (lda, 1) and a.shape[0] >= M and a.shape[1] >= w.K):
-            assert 2 * (a.storage_offset() + (M - 1) * lda + w.K) <= a.untyped_storage().nbytes(), "fewer rows than the call names"
+        if M is None and lda is None:
+            M, lda = a.shape[0], a.stride(0)
+            assert a.shape[1] >= w.K and a.stride(1) == 1, "rows of the matrix's inputs"
+        else:
+            M, lda = a.shape[0] if M is None else M, a.stride(0) if lda is None else lda
+            assert M <= 0 or 2 * (a.storage_offset() + (M - 1) * lda + w.K) <= a.untyped_storage().nbytes(), "fewer rows than the call names"
         assert out.dtype == (self.torch_dtype, torch.float32, self.operand_dtype)[epilogue] and out.numel() >= M * w.N
         self._check(self.lib.marche_linear_quantized(self.h, a.data_ptr(), lda, M, w.ref, _ptr(bias), epilogue, _ptr(out),
                                                      _stream(stream)))

@@ -280,7 +280,8 @@ gemm_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __gri
             for (int i = 0; i < C::DG; ++i)
 #pragma unroll
               for (int q = 0; q < NR; q += 16) tmem_ld_32x16(d_at + (uint32_t)((e * C::DG + i) * NR + q), x[i] + q);
-            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < C::DG; ++i) ptx::tmem_ld_wait(x[i]);
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar(B_D_EMPTY + e));

@@ -544,7 +544,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
             for (int qc = 0; qc < DH / 16; ++qc) {
               uint32_t ov[16];
               tmem_ld_32x16(t_o + (uint32_t)(qc * 16), ov);
-              ptx::tmem_ld_wait();
+              ptx::tmem_ld_wait(ov);
 #pragma unroll
               for (int c = 0; c < 16; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * fo);
               tmem_st_32x16(t_o + (uint32_t)(qc * 16), ov);
@@ -571,7 +571,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         for (int qc = 0; qc < DH / 16; ++qc) {
           uint32_t ov[16];
           tmem_ld_32x16(t_o + (uint32_t)(qc * 16), ov);
-          ptx::tmem_ld_wait();
+          ptx::tmem_ld_wait(ov);
           if (there) {
             uint32_t w[8];
 #pragma unroll

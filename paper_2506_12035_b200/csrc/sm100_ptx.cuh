@@ -201,10 +201,10 @@ MARCHE_DEVINL void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32]) {
 MARCHE_DEVINL void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // The wait, tied to the registers it makes valid: no use of them can move in front of it.
-MARCHE_DEVINL void tmem_ld_wait(uint32_t (&r)[32]) {
+template <int N> MARCHE_DEVINL void tmem_ld_wait(uint32_t (&r)[N]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
 
 // ---------------------------------------------------------------- 2-CTA (cta_group::2) forms
