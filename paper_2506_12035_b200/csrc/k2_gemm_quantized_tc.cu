@@ -7,7 +7,8 @@
 // fp32 registers, which are stored as whole lines at the end.
 // Persistent CTAs, one per SM, or pairs (a cluster) that split K where that divides the units more evenly: the halves' sums meet by st.async in the
 // CTA that owns the row (31 x 24576 x 12288, 192 units: 61 and 52 us).  Stages of 256 inputs; warps: 0-3 convert the even stages, 4-7 the odd ones, 8-11 add
-// up, 12 fetches, 13 and 14 issue MMAs of even and odd stages.  All waits are bounded and report through the status word.
+// up, 12 fetches, 13 and 14 issue MMAs of even and odd stages.  All waits are bounded and report through the status word (all but the allocation of tensor
+// memory, for which no cluster of another kernel can make a pair wait for good: kPairSmem).
 // What bounds it: the conversion's instructions (per 64 inputs of 32 outputs 48 integer ones at two cycles each and 32 packed FMAs), 1200 cycles a stage
 // where its bytes would take 700; half of the issue slots, 40 % of the integer pipe, and 72 stages on the busiest SM for 62 on average.
 // 31 x 24576 x 12288, group 128: 52 us of 25 for the bytes (3.0 TB/s); group 64 59 us, group 32 79 us (sums twice and four times as often).
@@ -28,6 +29,9 @@ constexpr int kOut = 128;                  // outputs of a unit
 constexpr int SC = 4;                      // chunks of a stage
 constexpr int kThreads = 15 * 32;
 constexpr int NST = 6;                     // stages (even: a stage and its slot are of one parity)
+// A pair waits for its partner with all tensor memory allocated: the other kernel whose clusters do such a thing is kept off its SM (kernels.h), in the
+// narrow forms by shared memory that is not used.
+constexpr int kPairSmem = 212 * 1024;
 enum { W_ACC = 8, W_PROD = 12, W_MMA = 13 };   // (and W_MMA + 1)
 enum { ST_GEMM_QUANTIZED_TC = 0x67 };
 enum { B_FULL = 0, B_EMPTY = B_FULL + NST, B_A_FULL = B_EMPTY + NST, B_A_EMPTY = B_A_FULL + 2, B_D_FULL = B_A_EMPTY + 2, B_D_EMPTY = B_D_FULL + 4, B_RECV = B_D_EMPTY + 4, NB = B_RECV + 2 };
@@ -39,6 +43,7 @@ template <int NR, int G> struct Cfg {
   static constexpr int STAGE = (ROWS + CODES + SCALES + 1023) / 1024 * 1024, FILL = ROWS + CODES + SCALES;
   static constexpr int RECV = 2 * (NR / 2) * kOut * 4;     // two units' halves
   static constexpr int SMEM = 1024 + NST * STAGE + RECV;
+  static constexpr int SMEM_PAIR = SMEM > kPairSmem ? SMEM : kPairSmem;
   static constexpr uint32_t COL_A = 0, COL_D = 2 * SC * 32, COLS = 512;   // A: two buffers of SC chunks, 32 columns each; D: four of DG groups of NR
 };
 
@@ -365,7 +370,8 @@ template <int NR, int G, bool BF>
 cudaError_t launch(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int epi, void* out, int out_bf16, int cs,
                    int* status, cudaStream_t st) {
   using C = Cfg<NR, G>;
-  static_assert(C::SMEM <= 226 * 1024, "shared memory of one CTA");
+  static_assert(C::SMEM_PAIR <= 226 * 1024 && keeps_clusters_out(C::SMEM_PAIR), "shared memory of one CTA");
+  const size_t smem = cs > 1 ? C::SMEM_PAIR : C::SMEM;
   CUtensorMap ta, tc, ts;
   EncodeTiledFn fn = tma_encode_fn();
   if (!fn) return cudaErrorInvalidValue;
@@ -386,12 +392,12 @@ cudaError_t launch(const void* a, int lda, int M, const void* codes, const void*
       !make(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, scales, ds, ss, bs, CU_TENSOR_MAP_SWIZZLE_NONE))
     return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
-  cudaError_t e = ensure_dynamic_smem(gemm_quantized_tc_kernel<NR, G, BF>, (size_t)C::SMEM, smem_set);
+  cudaError_t e = ensure_dynamic_smem(gemm_quantized_tc_kernel<NR, G, BF>, smem, smem_set);
   if (e != cudaSuccess) return e;
   Shape sh = {M, N, (int)chunks, (M + NR - 1) / NR, 0, cs, epi, out_bf16};
   sh.units = (N + kOut - 1) / kOut * sh.n_rb;
   const int most = device_sm_count() / cs, clusters = sh.units < most ? sh.units : most;
-  return launch_pdl_cluster(gemm_quantized_tc_kernel<NR, G, BF>, dim3((unsigned)(clusters * cs)), dim3(kThreads), (size_t)C::SMEM, cs, st, ta, tc, ts, bias, out, sh, status);
+  return launch_pdl_cluster(gemm_quantized_tc_kernel<NR, G, BF>, dim3((unsigned)(clusters * cs)), dim3(kThreads), smem, cs, st, ta, tc, ts, bias, out, sh, status);
 }
 
 template <int NR, bool BF>
@@ -403,6 +409,12 @@ cudaError_t by_group(const void* a, int lda, int M, const void* codes, const voi
 }
 
 }  // namespace
+
+size_t gemm_quantized_tc_smem(int M, int group, int cs) {
+  auto of = [&](auto c) { return (size_t)(cs > 1 ? decltype(c)::SMEM_PAIR : decltype(c)::SMEM); };
+  if (M <= 16) return group == 32 ? of(Cfg<16, 32>()) : group == 64 ? of(Cfg<16, 64>()) : of(Cfg<16, 128>());
+  return group == 32 ? of(Cfg<32, 32>()) : group == 64 ? of(Cfg<32, 64>()) : of(Cfg<32, 128>());
+}
 
 cudaError_t launch_gemm_quantized_tc(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group, int epilogue,
                                      void* out, bool a_bf16, int cs, int* status, cudaStream_t st) {

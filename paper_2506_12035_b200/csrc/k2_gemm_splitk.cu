@@ -334,32 +334,40 @@ gemm_splitk_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
   }
 }
 
-template <int BN, int CS, int EPI>
-cudaError_t launch_one(const CUtensorMap& ta, const CUtensorMap& tw, int M, int N, int K, int a_rows, const float* bias,
-                       void* out, const KvScatter& kv, int a_bf16, int* status, cudaStream_t st) {
-  const int n_tiles = ((M + BM - 1) / BM) * (N / BN);
-  const int fixed = 1024 + 256 + (CS > 1 ? BM * BN * 4 : BN * 4);
-  const int stage = a_rows * BK * 2 + BN * BK * 2;
-  const int n_it = (K / BK + CS - 1) / CS;
-  constexpr int budget = BN == 128 && CS > 1 ? kSmemBudgetWide : kSmemBudget;
-  int stages = (budget - fixed) / stage;
+constexpr int budget_of(int bn, int cs) { return bn == 128 && cs > 1 ? kSmemBudgetWide : kSmemBudget; }
+constexpr int fixed_of(int bn, int cs) { return 1024 + 256 + (cs > 1 ? BM * bn * 4 : bn * 4); }
+static_assert(fixed_of(32, 2) + (8 + 32) * BK * 2 >= kLeastSplitKSmem && fixed_of(64, 2) >= kLeastSplitKSmem, "one stage of eight rows");
+
+// The stages of a CTA's ring, its bytes, and all of the CTA's shared memory.
+struct Ring { int stages; size_t bytes, smem; };
+Ring ring_of(int bn, int cs, int a_rows, int K) {
+  const int fixed = fixed_of(bn, cs), stage = a_rows * BK * 2 + bn * BK * 2, n_it = (K / BK + cs - 1) / cs;
+  int stages = (budget_of(bn, cs) - fixed) / stage;
   if (stages > kMaxStages) stages = kMaxStages;
   if (stages > n_it) stages = n_it;
   // The MMA reads 128 rows of A from the last slot on, whatever they hold, and without a cluster the ring ends as the
   // epilogue's 32 KB of staging boxes.
   size_t ring = (size_t)stages * stage;
   const size_t reach = (size_t)(stages - 1) * a_rows * BK * 2 + BM * BK * 2;
-  if (CS > 1 ? reach > ring + BM * BN * 4 : reach > ring) ring = reach;
-  if (CS == 1 && ring < 32768) ring = 32768;
-  const size_t smem = fixed + ring;
+  if (cs > 1 ? reach > ring + BM * bn * 4 : reach > ring) ring = reach;
+  if (cs == 1 && ring < 32768) ring = 32768;
+  return {stages, ring, fixed + ring};
+}
+
+template <int BN, int CS, int EPI>
+cudaError_t launch_one(const CUtensorMap& ta, const CUtensorMap& tw, int M, int N, int K, int a_rows, const float* bias,
+                       void* out, const KvScatter& kv, int a_bf16, int* status, cudaStream_t st) {
+  const int n_tiles = ((M + BM - 1) / BM) * (N / BN);
+  const Ring r = ring_of(BN, CS, a_rows, K);
+  constexpr int budget = budget_of(BN, CS);
   OutMap<CS> to = {};
   if constexpr (CS == 1)
     if (!tma_make_store_map(&to, out, (uint64_t)M, (uint64_t)N, EPI == 1 ? 4 : 2)) return cudaErrorInvalidValue;
   static size_t smem_set[kMaxDevices] = {};
   cudaError_t e = ensure_dynamic_smem(gemm_splitk_kernel<BN, CS, EPI>, (size_t)budget, smem_set);
   if (e != cudaSuccess) return e;
-  return launch_pdl_cluster(gemm_splitk_kernel<BN, CS, EPI>, dim3(n_tiles * CS), dim3(kThreads), smem, CS, st, ta, tw, to, M, N,
-                            K, a_rows, stages, (int)ring, bias, out, kv, a_bf16, status);
+  return launch_pdl_cluster(gemm_splitk_kernel<BN, CS, EPI>, dim3(n_tiles * CS), dim3(kThreads), r.smem, CS, st, ta, tw, to, M, N,
+                            K, a_rows, r.stages, (int)r.bytes, bias, out, kv, a_bf16, status);
 }
 
 }  // namespace
@@ -391,6 +399,8 @@ double gemm_splitk_cost(int M, int N, int K, SplitKShape shape) {
   if (load > 1.0) t += 1.34;
   return bn == 128 ? t + 0.15 : t;
 }
+
+size_t gemm_splitk_smem(int M, int K, SplitKShape shape) { return ring_of(shape.bn, shape.cs, rows_per_tile(M, shape.cs), K).smem; }
 
 SplitKShape gemm_splitk_pick(int M, int N, int K) {
   static const SplitKShape shapes[] = {{64, 1}, {64, 2}, {64, 4}, {64, 8}, {32, 2}, {32, 4}, {128, 1}, {128, 2}, {128, 4}, {128, 8}};

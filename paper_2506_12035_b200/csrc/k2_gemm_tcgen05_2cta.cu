@@ -43,6 +43,7 @@ template <int BN> struct PairCfg {
   static constexpr int BIAS_BYTES = 2 * BN * 4;                  // one slot per accumulator
   static constexpr int SMEM_BYTES = RING_BYTES + STAGING_BYTES + BIAS_BYTES + 256;
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of one CTA");
+  static_assert(keeps_clusters_out(SMEM_BYTES), "the pair waits for its partner with its tensor memory allocated");
   static constexpr int TMEM_COLS = 2 * BN;
 };
 

@@ -94,6 +94,13 @@ double gemm_tcgen05_2cta_cost(int M, int N, int K, int bn);   // microseconds, f
 // shared memory (a cluster of cs CTAs).  Same operand rules; epilogue 4 takes any D that is a multiple of bn.
 struct SplitKShape { int bn, cs; };
 SplitKShape gemm_splitk_pick(int M, int N, int K);
+size_t gemm_splitk_smem(int M, int K, SplitKShape shape);           // shared memory of a CTA
+// A kernel whose clusters wait for one another while they hold tensor memory must not share an SM with another such kernel if their columns
+// together exceed 512: with one of each on two SMs, allocated in opposite orders (two streams), either would wait for a CTA that cannot
+// allocate, and an allocation has no limit after which it gives up.  The split-K clusters, of 32 to 128 columns and no less shared memory a column
+// than this, fit beside one another; a kernel that takes more columns leaves less shared memory on its SM than the smallest of them needs.
+constexpr int kSmSharedBytes = 228 * 1024, kCtaReservedBytes = 1024, kLeastSplitKSmem = 22784;
+constexpr bool keeps_clusters_out(int smem) { return kSmSharedBytes - (smem + kCtaReservedBytes) < kLeastSplitKSmem + kCtaReservedBytes; }
 double gemm_splitk_cost(int M, int N, int K, SplitKShape shape);   // microseconds, for the choice of a kernel
 cudaError_t launch_gemm_splitk(const void* a, int lda, int M, const void* w, const float* bias, int N, int K, int epilogue,
                                void* out, bool a_bf16, int* status, cudaStream_t st, SplitKShape shape,
@@ -193,6 +200,7 @@ size_t gemm_quantized_smem(int M, int group, const QuantizedGemmShape& s);
 cudaError_t launch_gemm_quantized(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
                                   int epilogue, void* out, bool a_bf16, int* status, cudaStream_t st);
 // The same on tcgen05, for large matrices; cs 1, or 2 for pairs of CTAs that split K.
+size_t gemm_quantized_tc_smem(int M, int group, int cs);
 cudaError_t launch_gemm_quantized_tc(const void* a, int lda, int M, const void* codes, const void* scales, const float* bias, int N, int K, int group,
                                      int epilogue, void* out, bool a_bf16, int cs, int* status, cudaStream_t st);
 cudaError_t launch_quantize_weights(const float* w, int N, int K, int group, void* codes, void* scales, cudaStream_t st);

@@ -107,3 +107,21 @@ def test_which_attention(lib, R, S, dh, items, want):
     wins = lib._ZN6marche27attention_quantized_tc_winsEiiii
     wins.restype = C.c_bool
     assert wins(R, S, dh, items) is want
+
+
+class SplitK(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("bn", "cs")]
+
+
+def test_pairs_that_hold_tensor_memory_share_no_sm_with_other_clusters(lib):
+    """A pair of the projections waits for its partner with all of its SM's tensor memory.  Clusters of another stream that hold some while they wait
+    would, beside it, each wait for the other for good: together they need more shared memory than an SM has (228 KB, 1 KB of it for each CTA)."""
+    pair, other = lib._ZN6marche22gemm_quantized_tc_smemEiii, lib._ZN6marche16gemm_splitk_smemEiiNS_11SplitKShapeE
+    pair.restype, pair.argtypes = C.c_size_t, [C.c_int] * 3
+    other.restype, other.argtypes = C.c_size_t, [C.c_int, C.c_int, SplitK]
+    least = min(other(M, 64 * chunks, SplitK(bn, cs)) for bn, cs in [(64, 2), (64, 4), (64, 8), (32, 2), (32, 4), (128, 2), (128, 4), (128, 8)]
+                for M in (1, 8, 9, 16, 100, 128, 129, 1000) for chunks in (cs, cs + 1, 12, 100) if chunks >= cs)
+    for M in (9, 16, 17, 32, 33, 65536):
+        for group in (32, 64, 128):
+            assert pair(M, group, 1) <= pair(M, group, 2) <= 227 * 1024, (M, group)
+            assert pair(M, group, 2) + 1024 + least + 1024 > 228 * 1024, (M, group)
