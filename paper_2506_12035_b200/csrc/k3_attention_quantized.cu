@@ -2,7 +2,7 @@
 //
 // o = softmax(q K^T / sqrt(dh)) V with K[s] = ks[s] ck[s], V[s] = vs[s] cv[s], codes c in -127 .. 127 and one scale per key and head.
 // The scales are kept out of the products: the logit of a key is ks[s] (q . ck[s]), and vs[s] goes into the weight, so the tensor
-// cores multiply the codes themselves, which are exact in fp16.  q (bf16) is exact in fp16 after a power of two is taken off; what
+// cores multiply the codes themselves, which are exact in fp16.  q (bf16) is exact in fp16 after a power of two of its row is taken off; what
 // is rounded is the weight: p vs / 2^e to fp16 (11 bits), where 2^e bounds the largest value scale met so far and the whole is
 // lifted by 2^14, so that a weight 2^-28 of the largest possible keeps all its bits.  Maxima, sums and accumulators are fp32, and the running
 // exponent e moves with the running maximum (one factor for both).
@@ -108,11 +108,6 @@ MARCHE_DEVINL void add2(float& a, float& b, float x, float y) {
   a = r.x;
   b = r.y;
 }
-MARCHE_DEVINL void fma2(float& a, float& b, float m, float x, float y) {   // a m + x, b m + y
-  const float2 r = __ffma2_rn(make_float2(a, b), make_float2(m, m), make_float2(x, y));
-  a = r.x;
-  b = r.y;
-}
 MARCHE_DEVINL float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -185,7 +180,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
     while (issued < mine && issued < sp.nst) load();
   __syncwarp();
 
-  // Rows 2 t and 2 t + 1 of each eight: running maximum (of the raw logits), this lane's part of the sum of weights; O^T: columns 16 c + 2 g (entries
+  // Rows 2 t and 2 t + 1 of each eight: running maximum (of the logits in units of log2), this lane's part of the sum of weights; O^T: columns 16 c + 2 g (entries
   // 0, 1 for the two rows) and 16 c + 2 g + 1 (2, 3).
   bool ok = true;
   const bool active = row_w < R;
@@ -200,29 +195,32 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
   }
   // ---- the warp's query rows as the operand of eight columns: lane (g, t) holds row g's values 0, 2 and 1, 3 of each step's four
   uint32_t qf[NB][C::STEPS][2];
-  float c_log2 = 0.f, q_off[NB][2];
+  float c_log2[NB][2], q_off[NB][2];                       // of rows 2 t and 2 t + 1 of each eight
   if (active) {
     uint2 x[NB][C::STEPS];
-    uint32_t top = 0;
 #pragma unroll
     for (int m = 0; m < NB; ++m) {
       const int row = min(row_w + 8 * m + g, R - 1), token = row / G;       // (rows behind the last are the last one again: not stored)
       const bf16* src = q + ((size_t)b * n + token) * ld_q + (h * G + row - token * G) * DH;
 #pragma unroll
-      for (int s = 0; s < C::STEPS; ++s) {
-        x[m][s] = *reinterpret_cast<const uint2*>(src + value_of<DH>(s, t));
-        const uint32_t big = max(max(x[m][s].x & 0x7fffu, (x[m][s].x >> 16) & 0x7fffu), max(x[m][s].y & 0x7fffu, (x[m][s].y >> 16) & 0x7fffu));
-        top = max(top, big < 0x7f80u ? big : 0u);          // (infinities and NaN stay what they are, in their row)
-      }
+      for (int s = 0; s < C::STEPS; ++s) x[m][s] = *reinterpret_cast<const uint2*>(src + value_of<DH>(s, t));
     }
-    top = __reduce_max_sync(0xffffffffu, top);
-    // All rows divided by the largest value's power of two and lifted by 2^15, fp16's largest (a bf16 number below 2 stays below 65504): exact
-    // down to 2^-30 of the largest value, and no logit is off by more than 2^-40 of the largest ones'.
-    const int e = min(max((int)(top >> 7), 16), 254);
-    const float f = pow2(269 - e), scale_log2 = rsqrtf((float)DH) * 1.4426950408889634f;
-    c_log2 = scale_log2 * pow2(e);                          // (codes as subnormals: 2^24 over 2^15, the rest goes to the keys' scales)
+    const float scale_log2 = rsqrtf((float)DH) * 1.4426950408889634f;
 #pragma unroll
     for (int m = 0; m < NB; ++m) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int s = 0; s < C::STEPS; ++s) {
+        const uint32_t big = max(max(x[m][s].x & 0x7fffu, (x[m][s].x >> 16) & 0x7fffu), max(x[m][s].y & 0x7fffu, (x[m][s].y >> 16) & 0x7fffu));
+        top = max(top, big < 0x7f80u ? big : 0u);          // (infinities and NaN stay what they are)
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));   // of row g
+      // The row divided by its largest value's power of two and lifted by 2^15, fp16's largest (a bf16 number below 2 stays below 65504): exact
+      // down to 2^-32 of the largest value, and no logit is off by more than 2^-40 of its row's largest ones'.  Each row by its own: a row of padding
+      // may hold numbers of any size.
+      const int e = min(max((int)(top >> 7), 16), 254);
+      const float f = pow2(269 - e), c = scale_log2 * pow2(e);   // (codes as subnormals: 2^24 over 2^15, the rest goes to the keys' scales)
       float sum = 0.f;
 #pragma unroll
       for (int s = 0; s < C::STEPS; ++s) {
@@ -237,6 +235,8 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
       sum *= -128.0f * 0x1p-24f;
       q_off[m][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
       q_off[m][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+      c_log2[m][0] = __shfl_sync(0xffffffffu, c, 8 * t);
+      c_log2[m][1] = __shfl_sync(0xffffffffu, c, 8 * t + 4);
     }
   }
   int turn = 0, phase = 0, turn_before = 0, phase_before = 0;   // stage of tile u in the group's ring, its fill's parity; the tile's before it
@@ -290,9 +290,9 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
         f0 *= 512.0f;                                      // (2^24 over the rows' 2^15)
         f1 *= 512.0f;
 #pragma unroll
-        for (int m = 0; m < NB; ++m) {
-          mul2(sacc[m][i][0], sacc[m][i][1], f0, f0);
-          mul2(sacc[m][i][2], sacc[m][i][3], f1, f1);
+        for (int m = 0; m < NB; ++m) {                     // in units of log2
+          mul2(sacc[m][i][0], sacc[m][i][1], f0 * c_log2[m][0], f0 * c_log2[m][1]);
+          mul2(sacc[m][i][2], sacc[m][i][3], f1 * c_log2[m][0], f1 * c_log2[m][1]);
         }
       }
       if (left < KT) {
@@ -325,10 +325,10 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
           const float ref = mx == -INFINITY ? 0.f : mx;
-          corr[m][r] = ex2_approx((m_run[m][r] - ref) * c_log2);
+          corr[m][r] = ex2_approx(m_run[m][r] - ref);
           moved = moved || mx != m_run[m][r];
           m_run[m][r] = mx;
-          neg[m][r] = -ref * c_log2;
+          neg[m][r] = -ref;
         }
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
@@ -356,7 +356,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
             float p0 = sacc[m][i][2 * hf], p1 = sacc[m][i][2 * hf + 1];
-            fma2(p0, p1, c_log2, neg[m][0], neg[m][1]);
+            add2(p0, p1, neg[m][0], neg[m][1]);
             p0 = ex2_approx(p0);
             p1 = ex2_approx(p1);
             add2(ls[m][0], ls[m][1], p0, p1);
@@ -462,8 +462,8 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
           for (int c = 0; c < C::CHUNKS; ++c)
             asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * (16 * c + 2 * g)), "f"(oacc[m][c][r] * unlift),
                          "f"(oacc[m][c][2 + r] * unlift) : "memory");
-          if (g == 0)                                      // the maximum in the exponent's own units
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * DH), "f"(m_run[m][r] * c_log2), "f"(l_run[m][r]) : "memory");
+          if (g == 0)
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * DH), "f"(m_run[m][r]), "f"(l_run[m][r]) : "memory");
         }
       }
   }

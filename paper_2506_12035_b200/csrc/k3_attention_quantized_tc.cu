@@ -9,7 +9,7 @@
 //   4  softmax, one thread per row: logits from tensor memory times the keys' scales less the running reference (it moves only when a tile
 //      exceeds it by 2^8, so that one packed FMA per pair is all before the exponential), weights times value scales packed to fp16 and
 //      written back to tensor memory as the A operand of P V
-//   2  converters: the unit's query rows (fp16, all divided by the power of two of the largest), then per tile K and V from bytes to swizzled
+//   2  converters: the unit's query rows (fp16, divided by a power of two), then per tile K and V from bytes to swizzled
 //      fp16 operand tiles (two of each), the scales, and the running exponent above all value scales, which the weights are relative
 //      to.  (Four of them, or a third stream, take registers from the softmax: 484 and 492 us where two streams of two took 424.)
 //   1  TMA producer: codes and scales of the tiles into a staging ring
@@ -35,7 +35,7 @@ enum { ST_ATT_QUANTIZED_TC = 0x53 };
 // barriers of one stream
 enum { B_STG_FULL = 0, B_STG_EMPTY = B_STG_FULL + NSTG, B_K_FULL = B_STG_EMPTY + NSTG, B_K_EMPTY = B_K_FULL + NB2, B_V_FULL = B_K_EMPTY + NB2,
        B_V_EMPTY = B_V_FULL + NB2, B_SC_FULL = B_V_EMPTY + NB2, B_Q_FULL = B_SC_FULL + NSC, B_TOP, B_Q_EMPTY, B_S_FULL, B_S_FREE, B_P_FULL, B_O_FULL, NB };
-constexpr int kScaleSlot = 2 * KT + 4;     // floats: ks in units of log2 [64], vs lifted [64], step, unlift
+constexpr int kScaleSlot = 2 * KT + 4;     // words: ks in units of log2 [64], vs lifted [64], step, unlift, 1 + buffer of the rows' own factors (0: none)
 
 template <int DH, int NS> struct Cfg {
   static constexpr int NC = 2;                             // converters of a stream
@@ -50,7 +50,8 @@ template <int DH, int NS> struct Cfg {
   static constexpr int OFF_Q = 0, OFF_K = OFF_Q + NS * Q_BYTES, OFF_V = OFF_K + NS * NB2 * T_BYTES, OFF_STG = OFF_V + NS * NB2 * T_BYTES;
   static constexpr int OFF_RAW = OFF_STG + NS * NSTG * STG_BYTES;          // scales as they come: [stream][slot][2 KT]
   static constexpr int OFF_SC = OFF_RAW + NS * NSTG * 2 * KT * 4, OFF_ROW = OFF_SC + NS * NSC * kScaleSlot * 4;
-  static constexpr int OFF_BAR = OFF_ROW + NS * 32;                        // largest value of each converter's rows
+  static constexpr int OFF_FACTOR = OFF_ROW + NS * 32;                     // largest and smallest value of each converter's rows
+  static constexpr int OFF_BAR = OFF_FACTOR + NS * 2 * QT * 4;             // the rows' own powers of two: [stream][units in turn][row]
   static constexpr int OFF_MISC = OFF_BAR + 8 * NS * NB, SMEM_BYTES = OFF_MISC + 32 + 1024;
   static_assert(NS * COL_STREAM <= TMEM_COLS && SMEM_BYTES <= 227 * 1024 && OFF_BAR % 8 == 0 && OFF_SC % 16 == 0 && (kScaleSlot * 4) % 16 == 0, "budgets of a CTA");
   static_assert(T_BYTES % 1024 == 0 && Q_BYTES % 1024 == 0 && STG_BYTES % 1024 == 0 && OFF_RAW % 16 == 0, "alignment of operand tiles");
@@ -95,6 +96,15 @@ MARCHE_DEVINL void tmem_st_32x16(uint32_t taddr, const uint32_t* r) {
       : "memory");
 }
 MARCHE_DEVINL void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 16 columns of a row in tensor memory times f.
+MARCHE_DEVINL void scale_in_place(uint32_t taddr, float f) {
+  uint32_t v[16];
+  tmem_ld_32x16(taddr, v);
+  ptx::tmem_ld_wait(v);
+#pragma unroll
+  for (int c = 0; c < 16; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * f);
+  tmem_st_32x16(taddr, v);
+}
 MARCHE_DEVINL float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -320,13 +330,17 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
     for (int u = 0; u < n_units && ok; ++u) {
       const Unit un = unit_of<NS>(j, u, deal, sh, kv_len);
       if (un.n_kv == 0) continue;
-      // ---- the unit's rows, one per lane at a time: in fp16, all divided by the largest value's power of two and lifted by 2^15 (a bf16 number below 2
-      // stays below fp16's end; no logit is off by more than 2^-40 of the largest ones'); the loads are under way while the last unit's S is
+      // ---- the unit's rows, one per lane at a time: in fp16, divided by a power of two and lifted by 2^15 (a bf16 number below 2 stays below fp16's
+      // end); the loads are under way while the last unit's S is.  The power is that of the unit's largest value where that keeps all bits of
+      // all values (down to 2^-32 of it), so that it goes into the keys' scales.  Elsewhere (a row of padding may hold numbers of any size)
+      // each row has its own, no logit of it is off by more than 2^-40 of its largest ones', and its softmax thread multiplies its products by
+      // it.  Both give the same bits: no row depends on another.
       float c_log2;
+      bool own;
       {
         constexpr int ROWS = QT / NC / 32;                 // of a lane
         uint4 x[ROWS][DH / 8];
-        uint32_t top = 0;
+        uint32_t top[ROWS], low = 0xffffffffu;             // largest finite one of each row; smallest of all that are not 0, less 1
 #pragma unroll
         for (int p = 0; p < ROWS; ++p) {
           const int row = un.row0 + part * (QT / NC) + p * 32 + lane, token = row / sh.G;
@@ -336,31 +350,48 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
           for (int c = 0; c < DH / 8; ++c) x[p][c] = there ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-        for (int p = 0; p < ROWS; ++p)
+        for (int p = 0; p < ROWS; ++p) {
+          top[p] = 0;
 #pragma unroll
           for (int c = 0; c < DH / 8; ++c) {
             const uint32_t w[4] = {x[p][c].x, x[p][c].y, x[p][c].z, x[p][c].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {                  // (infinities and NaN stay what they are, in their row)
               const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;
-              top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+              top[p] = max(top[p], max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+              low = min(low, min(lo - 1u, hi - 1u));
             }
           }
-        top = __reduce_max_sync(0xffffffffu, top);
+        }
+        uint32_t all = top[0];
+#pragma unroll
+        for (int p = 1; p < ROWS; ++p) all = max(all, top[p]);
+        all = __reduce_max_sync(0xffffffffu, all);
+        low = __reduce_min_sync(0xffffffffu, low);
         // (two buffers: who writes a buffer again has passed the barrier of the unit between, which all reach after reading)
         volatile uint32_t* tops = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_ROW) + (j * 2 + (qn & 1)) * 4;
-        if (lane == 0) tops[part] = top;
+        if (lane == 0) {
+          tops[part] = all;
+          tops[NC + part] = low;
+        }
         __syncwarp();
         arrive(B_TOP);
         if (!wait(B_TOP, (uint32_t)qn & 1u)) { ok = false; break; }
 #pragma unroll
-        for (int p = 0; p < NC; ++p) top = max(top, tops[p]);
-        const int e = min(max((int)(top >> 7), 16), 254);
-        const float f = pow2(269 - e);
-        c_log2 = rsqrtf((float)DH) * 1.4426950408889634f * pow2(e - 15);
+        for (int p = 0; p < NC; ++p) {
+          all = max(all, tops[p]);
+          low = min(low, tops[NC + p]);
+        }
+        const int e = min(max((int)(all >> 7), 16), 254);
+        own = (int)((low + 1u) >> 7) + 32 < e || e > 191;  // (above: the scales' products with it could leave the range for a smaller row)
+        c_log2 = rsqrtf((float)DH) * 1.4426950408889634f * (own ? 256.0f : pow2(e - 15));
+        float* factors = reinterpret_cast<float*>(gen + C::OFF_FACTOR) + (j * 2 + (qn & 1)) * QT + part * (QT / NC) + lane;
         if (!wait(B_Q_EMPTY, ((uint32_t)qn & 1u) ^ 1u)) { ok = false; break; }
 #pragma unroll
-        for (int p = 0; p < ROWS; ++p)
+        for (int p = 0; p < ROWS; ++p) {
+          const int e_row = own ? min(max((int)(top[p] >> 7), 24), 254) : e;
+          const float f = pow2(269 - e_row);
+          if (own) factors[p * 32] = pow2(e_row - 23);     // (2^8 of it is in the scales: a row's products with its codes stay in range)
 #pragma unroll
           for (int c = 0; c < DH / 8; ++c) {
             const uint32_t w[4] = {x[p][c].x, x[p][c].y, x[p][c].z, x[p][c].w};
@@ -372,6 +403,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
             }
             *reinterpret_cast<uint4*>(q_tile + operand_off<DH>(QT, part * (QT / NC) + p * 32 + lane, c)) = make_uint4(y[0], y[1], y[2], y[3]);
           }
+        }
       }
       ptx::fence_proxy_async();
       __syncwarp();
@@ -415,6 +447,8 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         if (part == 0 && lane == 0) {
           scale_slot[2 * KT] = e_new == e_run || kt == 0 ? 1.f : (e_new - e_run > 120 ? 0.f : pow2(127 - (e_new - e_run)));
           scale_slot[2 * KT + 1] = pow2(e_new - 6);
+          // (two buffers: who writes a row's factor for the unit after next has seen this unit's S taken out of tensor memory)
+          scale_slot[2 * KT + 2] = __int_as_float(own ? 1 + ((qn - 1) & 1) : 0);
         }
         e_run = e_new;
         __syncwarp();
@@ -459,13 +493,21 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         ptx::tc_fence_after();
         const float4* ks4 = reinterpret_cast<const float4*>(gen + C::OFF_SC + (j * NSC + sc) * kScaleSlot * 4);
         const float4* vs4 = ks4 + KT / 4;
-        const float step = ks4[KT / 2].x;
-        unlift = ks4[KT / 2].y;
+        const float4 of_tile = ks4[KT / 2];
+        const float step = of_tile.x;
+        const int own = __float_as_int(of_tile.z);
+        unlift = of_tile.y;
         if (++sc == NSC) { sc = 0; sc_phase ^= 1u; }
         const int lim = un.len - i * KT;                   // keys of this tile that exist
         // The previous P V of this unit has read its weights and added to O.  (Without it no warp may announce this tile's weights.)
         auto previous_done = [&]() { return i == 0 || wait(B_O_FULL, (uint32_t)(t - 1) & 1u); };
         if (warp_valid) {
+          if (own) {                                       // (in place, so that units that need none of it pay a branch)
+            const float power = *(reinterpret_cast<const float*>(gen + C::OFF_FACTOR) + (2 * j + own - 1) * QT + r);
+#pragma unroll 1
+            for (int qc = 0; qc < KT / 16; ++qc) scale_in_place(t_s + (uint32_t)(qc * 16), power);
+            tmem_st_wait();
+          }
           uint32_t va[KT / 2], vb[KT / 2];                 // logits of the first and second 32 keys
           ptx::tmem_ld_32x32(t_s, va);
           ptx::tmem_ld_32x32(t_s + KT / 2, vb);
@@ -541,14 +583,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
             // this row's accumulator in tensor memory moves to the new references
             const float fo = f * step;
 #pragma unroll 1
-            for (int qc = 0; qc < DH / 16; ++qc) {
-              uint32_t ov[16];
-              tmem_ld_32x16(t_o + (uint32_t)(qc * 16), ov);
-              ptx::tmem_ld_wait(ov);
-#pragma unroll
-              for (int c = 0; c < 16; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * fo);
-              tmem_st_32x16(t_o + (uint32_t)(qc * 16), ov);
-            }
+            for (int qc = 0; qc < DH / 16; ++qc) scale_in_place(t_o + (uint32_t)(qc * 16), fo);
           }
           l = fmaf(l, f, (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
           tmem_st_wait();

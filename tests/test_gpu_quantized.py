@@ -662,3 +662,38 @@ def test_refusals(models):
         m.attention_quantized(rows, D + 8, n, H, cache, torch.zeros(1, dtype=torch.int32, device="cuda"), out)
     with pytest.raises(AssertionError):
         QuantizedCache(cache.codes, cache.scales[..., :32].contiguous(), H)
+
+
+# ------------------------------------------------------------------ rows, keys and sizes that have nothing to do with one another
+@pytest.mark.parametrize("dh,heads,kv_heads", [(64, 2, 2), (64, 8, 2), (80, 3, 3), (128, 4, 2)])
+@pytest.mark.parametrize("n", [1, 3, 20, 140])
+@pytest.mark.parametrize("operand", ["f16", "bf16"])
+def test_a_query_row_does_not_reach_other_rows(models, both_kernels, operand, dh, heads, kv_heads, n):
+    """Rows of padding may hold any finite numbers: the rows beside them keep their results, bit for bit."""
+    m, gen, B, S = models[operand], gen_of(n + dh + heads), 3, 333
+    cache = filled_cache(m, gen, B, S, kv_heads, dh)
+    q = randn(gen, B * n, heads, dh).to(torch.bfloat16)
+    want = attend(m, cache, q.view(B * n, -1), heads * dh, n, heads, None).view(B * n, heads, dh)
+    assert_attention(want, cache, q.view(B * n, -1), n, heads, None)
+    for power, at in [(33, -1), (60, 0), (120, n // 2), (60, 2 * n - 1)]:
+        other = q.clone()
+        if power == 60:
+            other[at, heads - 1] *= 2.0 ** power                     # one row of one head
+        else:
+            other[at, heads // 2, 5] = -3 * 2.0 ** power             # one value of it
+        o = attend(m, cache, other.view(B * n, -1), heads * dh, n, heads, None).view(B * n, heads, dh)
+        same_row = (other == q).all(-1)
+        assert int((~same_row).sum()) == 1
+        assert torch.equal(o[same_row], want[same_row]), (power, at)
+        assert bool(o.isfinite().all())
+
+
+@pytest.mark.parametrize("n", [2, 40, 140])
+def test_rows_of_all_sizes_side_by_side(models, both_kernels, n):
+    """Rows from 2^-100 to 2^6, a power of two apart, and rows whose own values are 2^45 apart."""
+    m, gen, B, S, H, dh = models["f16"], gen_of(n), 2, 200, 3, 64
+    cache = filled_cache(m, gen, B, S, H, dh)
+    q = randn(gen, B * n, H, dh) * torch.exp2(torch.randint(-100, 7, (B * n, H, 1), generator=gen, device="cuda").float() * (torch.rand(B * n, H, 1, generator=gen, device="cuda") < 0.7))
+    q[::3, :, ::2] *= 2.0 ** -45
+    q = (q / q.abs().amax(-1, keepdim=True).clamp_min(6.0) * 6.0).to(torch.bfloat16).view(B * n, H * dh)
+    assert_attention(attend(m, cache, q, H * dh, n, H, None), cache, q, n, H, None)
