@@ -14,11 +14,11 @@
 // mma.sync m16n8k16 on the transposed products, S^T = K q^T and O^T = V^T P^T: keys (then columns of V) are the 16-row operand and the
 // query rows come in eights, so one token costs half of what a 16-row tile of queries would, and the codes, converted once, serve all
 // NB eights of a warp.  K: a dot product does not mind the order of its terms, so a lane's 16 consecutive bytes of a key serve as its
-// operands of four k16 steps (bytes 0 and 2 of a word, then 1 and 3): no transposition and one shared-memory load; code + 128 as it
-// stands is a fp16 subnormal, (code + 128) 2^-24, which the tensor cores multiply exactly, and 128 times the sum of q is in the accumulator
-// beforehand.  V: ldmatrix.trans on pairs of bytes, whose even and odd bytes are rows g and g + 8 of the operand; here the sum over all keys would
-// leave too little of the result behind 128 times the weights' sum, so codes become numbers (1024 + code + 128, minus 1152).  P: the
-// accumulator's layout is turned by movmatrix.
+// operands of four k16 steps (bytes 0 and 2 of a word, then 1 and 3): no transposition and one shared-memory load.  V: ldmatrix.trans on
+// pairs of bytes, whose even and odd bytes are rows g and g + 8 of the operand.  Codes become numbers (1024 + code + 128, minus 1152); as they
+// stand, code + 128 is a fp16 subnormal, which the tensor cores multiply exactly, but 128 times the sum of the other operand would
+// have to come off, and where that is of one sign the result loses as many bits as it is smaller (for K too: logits off by 2^-16 of the sum of
+// magnitudes where fp32 sums are by 2^-23; 128 x 43 rows 2 % slower, one token over 65521 keys 3 %).  P: the accumulator's layout is turned by movmatrix.
 // nr warps take 8 NB rows each; nk groups of them take the tiles of 32 or 64 keys (K, V and both scales, by TMA) in turn, each group with a
 // ring of nst stages that its first warp fills (slot and phase are stepped: a division in that place cost more than the tile); a cluster of cs
 // CTAs splits a long sequence.  (CTA, group) pairs merge in rank order in the CTA that owns the row: bit-reproducible.  A sample without
@@ -75,13 +75,6 @@ MARCHE_DEVINL void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Bytes 0 and 2 (1 and 3) of a word of codes as fp16 subnormals, (code + 128) 2^-24.
-MARCHE_DEVINL uint32_t even_codes(uint32_t w) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0x28;" : "=r"(r) : "r"(w), "r"(0x80808080u), "r"(0x00ff00ffu));   // (w ^ 80..) & 00ff..
-  return r;
-}
-MARCHE_DEVINL uint32_t odd_codes(uint32_t w) { return even_codes(w >> 8); }
 // Two of the four bytes of a word of codes + 128 (SEL picks them and puts 0x64 above each) as fp16: 1024 + (code + 128) - 1152.
 template <uint32_t SEL> MARCHE_DEVINL uint32_t two_of(uint32_t biased) {
   uint32_t r;
@@ -195,7 +188,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
   }
   // ---- the warp's query rows as the operand of eight columns: lane (g, t) holds row g's values 0, 2 and 1, 3 of each step's four
   uint32_t qf[NB][C::STEPS][2];
-  float c_log2[NB][2], q_off[NB][2];                       // of rows 2 t and 2 t + 1 of each eight
+  float c_log2[NB][2];                                     // of rows 2 t and 2 t + 1 of each eight
   if (active) {
     uint2 x[NB][C::STEPS];
 #pragma unroll
@@ -220,21 +213,13 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
       // down to 2^-32 of the largest value, and no logit is off by more than 2^-40 of its row's largest ones'.  Each row by its own: a row of padding
       // may hold numbers of any size.
       const int e = min(max((int)(top >> 7), 16), 254);
-      const float f = pow2(269 - e), c = scale_log2 * pow2(e);   // (codes as subnormals: 2^24 over 2^15, the rest goes to the keys' scales)
-      float sum = 0.f;
+      const float f = pow2(269 - e), c = scale_log2 * pow2(e - 15);
 #pragma unroll
       for (int s = 0; s < C::STEPS; ++s) {
         const float2 lo = unpack_bf16x2(x[m][s].x), hi = unpack_bf16x2(x[m][s].y);
         qf[m][s][0] = pack_weights(lo.x * f, hi.x * f);
         qf[m][s][1] = pack_weights(lo.y * f, hi.y * f);
-        const float2 u = unpack_f16x2(qf[m][s][0]), v = unpack_f16x2(qf[m][s][1]);
-        sum += (u.x + u.y) + (v.x + v.y);
       }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);         // of row g
-      sum *= -128.0f * 0x1p-24f;
-      q_off[m][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
-      q_off[m][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
       c_log2[m][0] = __shfl_sync(0xffffffffu, c, 8 * t);
       c_log2[m][1] = __shfl_sync(0xffffffffu, c, 8 * t + 4);
     }
@@ -276,19 +261,15 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
           }
         }
 #pragma unroll
-        for (int m = 0; m < NB; ++m) {
-          sacc[m][i][0] = sacc[m][i][2] = q_off[m][0];
-          sacc[m][i][1] = sacc[m][i][3] = q_off[m][1];
-        }
+        for (int m = 0; m < NB; ++m) sacc[m][i][0] = sacc[m][i][1] = sacc[m][i][2] = sacc[m][i][3] = 0.f;
 #pragma unroll
         for (int k = 0; k < C::STEPS; ++k) {
-          const uint32_t a[4] = {even_codes(w0[k]), even_codes(w1[k]), odd_codes(w0[k]), odd_codes(w1[k])};
+          const uint32_t lo = w0[k] ^ 0x80808080u, hi = w1[k] ^ 0x80808080u;
+          const uint32_t a[4] = {two_of<0x4240>(lo), two_of<0x4240>(hi), two_of<0x4341>(lo), two_of<0x4341>(hi)};
 #pragma unroll
           for (int m = 0; m < NB; ++m) mma_f16(sacc[m][i], a, qf[m][k][0], qf[m][k][1]);
         }
-        float f0 = ks[key], f1 = ks[key + 8];
-        f0 *= 512.0f;                                      // (2^24 over the rows' 2^15)
-        f1 *= 512.0f;
+        const float f0 = ks[key], f1 = ks[key + 8];
 #pragma unroll
         for (int m = 0; m < NB; ++m) {                     // in units of log2
           mul2(sacc[m][i][0], sacc[m][i][1], f0 * c_log2[m][0], f0 * c_log2[m][1]);

@@ -697,3 +697,38 @@ def test_rows_of_all_sizes_side_by_side(models, both_kernels, n):
     q[::3, :, ::2] *= 2.0 ** -45
     q = (q / q.abs().amax(-1, keepdim=True).clamp_min(6.0) * 6.0).to(torch.bfloat16).view(B * n, H * dh)
     assert_attention(attend(m, cache, q, H * dh, n, H, None), cache, q, n, H, None)
+
+
+@pytest.mark.parametrize("dh", [64, 80, 128])
+@pytest.mark.parametrize("n,S", [(1, 9), (20, 9), (20, 150), (140, 150)])
+def test_rows_of_one_sign_over_small_codes(models, both_kernels, dh, n, S):
+    """One channel of K is large, so that the others' codes are small, and no row has anything there: a logit is a sum of small products, and only
+    they may round.  8 steps of the tensor cores at most, 2^-23 of the sum of magnitudes each, and three roundings of 2^-24: 2^-19.5 of it; a
+    weight is off by that share of itself, once for its own logit and once for the sum's."""
+    m, gen, B, H = models["f16"], gen_of(n), 12, 4
+    x = randn(gen, 2, B, S, H, dh)
+    x[0, ..., 3] = 100 * (1 + torch.rand(B, S, H, generator=gen, device="cuda"))
+    c, s = definition(x.to(torch.bfloat16))
+    cache = m.alloc_quantized_cache(B, S, H, dh)
+    cache.codes.copy_(c.to(torch.int8).view_as(cache.codes))
+    cache.scales[..., :S] = s.transpose(2, 3)
+    q = 6 * randn(gen, B * n, H, dh).abs()
+    q[..., 3] = 0
+    q = q.to(torch.bfloat16).view(B * n, H * dh)
+    o = attend(m, cache, q, H * dh, n, H, None).double().view(B * n, H, dh)
+    want, A, low = reference(cache, q, n, H, None)
+    size = torch.einsum("bnhd,bshd->bnhs", q.double().view(B, n, H, dh), values(cache)[0].abs()).amax(-1).view(B * n, H, 1) / dh ** 0.5
+    rounding = 2.0 ** -11 if both_kernels == "tcgen05" else 2.0 ** -22        # of the weights
+    limit = (rounding + 2 * 2.0 ** -19.5 * size) * A + low + HALF[torch.float16] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -24
+    assert bool(((o - want).abs() <= limit).all()), "error %.3g of the bound" % float(((o - want).abs() / limit).max())
+
+
+def test_keys_at_the_upper_end_of_the_range(models, both_kernels):
+    """K near the largest bf16 number and rows near the smallest: the logits are ordinary."""
+    m, gen, B, S, H, dh = models["bf16"], gen_of(12), 1, 200, 2, 64
+    cache = filled_cache(m, gen, B, S, H, dh, spread=False)
+    cache.scales[0] *= 2.0 ** 124                                     # up to 2^120 a code
+    assert float(cache.scales[0, :, :, :S].max()) > 2.0 ** 119 and bool((127 * cache.scales[0, :, :, :S]).isfinite().all())
+    for n in (3, 140):
+        q = (randn(gen, B * n, H * dh) * 2.0 ** -121).to(torch.bfloat16)
+        assert_attention(attend(m, cache, q, H * dh, n, H, None), cache, q, n, H, None)
