@@ -4,8 +4,8 @@
 // The scales are kept out of the products: the logit of a key is ks[s] (q . ck[s]), and vs[s] goes into the weight, so the tensor
 // cores multiply the codes themselves, which are exact in fp16.  q (bf16) is exact in fp16 after a power of two of its row is taken off; what
 // is rounded is the weight: p vs / 2^e to fp16 (11 bits), where 2^e bounds the largest value scale met so far and the whole is
-// lifted by 2^14, so that a weight 2^-28 of the largest possible keeps all its bits.  Maxima, sums and accumulators are fp32, and the running
-// exponent e moves with the running maximum (one factor for both).
+// lifted by 2^14, so that a weight 2^-28 of the largest possible keeps all its bits (scales far apart: attention_quantized.cuh).  Maxima, sums and
+// accumulators are fp32, and the running exponent e moves with the running maximum (one factor for both).
 // Where the output is fp16, what that rounding left off follows as a second operand (FINE): with one rounding of as many bits as the output's own the
 // error is 1.4 times the output's, 1.55 over few keys.  A bf16 output, eight times coarser, does not need it (128 x 43 rows over 320 keys of 16
 // heads of 80: 64 us without, 72 with it).
@@ -29,6 +29,7 @@
 #include <cuda.h>
 
 #include "attention_common.cuh"
+#include "attention_quantized.cuh"
 #include "kernels.h"
 #include "launch_pdl.h"
 #include "sm100_ptx.cuh"
@@ -40,9 +41,11 @@ namespace {
 
 using att::ex2_approx;
 using att::ldsm_x4_trans;
+using attq::pow2;
 
 constexpr int kMaxStages = 16;             // of a CTA
 constexpr int kThreadsMax = 256;
+constexpr int kSpread = 16;                // a row's largest product is at least 2^(14 - 1 - 16) before its sample counts as wide
 enum { ST_ATTENTION_QUANTIZED = 0x25 };
 
 // Keys per tile: 64 where shared memory holds two tiles for each of eight warps.
@@ -111,7 +114,6 @@ MARCHE_DEVINL uint32_t turn8x8(uint32_t x) {               // an 8 x 8 matrix of
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-MARCHE_DEVINL float pow2(int biased_exponent) { return __int_as_float(biased_exponent << 23); }
 
 // Grid: B * H * n_rb * cs CTAs, the cs of a cluster next to one another.
 template <int DH, int NB, bool FINE>
@@ -178,7 +180,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
   bool ok = true;
   const bool active = row_w < R;
   float m_run[NB][2], l_run[NB][2], oacc[NB][C::CHUNKS][4];
-  int e_run = 14;                                          // biased exponent above every value scale so far (14: the lowest whose factors exist)
+  attq::Units units;
 #pragma unroll
   for (int m = 0; m < NB; ++m) {
     m_run[m][0] = m_run[m][1] = -INFINITY;
@@ -285,36 +287,55 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
             if (16 * i + g + 8 >= left) sacc[m][i][2] = sacc[m][i][3] = -INFINITY;
           }
       }
-      // ---- references: the largest value scale (they are not negative: they order as integers; NaN counts as the largest number), the rows' maxima
-      uint32_t top = __float_as_uint(vs[lane]);
-      if (KT == 64) top = max(top, __float_as_uint(vs[lane + KT / 2]));
-      top = __reduce_max_sync(0xffffffffu, top);
-      const int e_new = max(e_run, min((int)(top >> 23), 254));
-      const float lift = pow2(267 - e_new);                // 2^14 over the power of two above the scale
-      const float step = e_new == e_run ? 1.f : (e_new - e_run > 120 ? 0.f : pow2(127 - (e_new - e_run)));
-      e_run = e_new;
-      float neg[NB][2], corr[NB][2];
-      bool moved = step != 1.f;
+      // ---- references: the unit above the value scales, the rows' maxima
+      const uint32_t v0 = __float_as_uint(vs[lane]), v1 = KT == 64 ? __float_as_uint(vs[lane + KT / 2]) : v0;
+      const int d = units.take<kSpread>(__reduce_max_sync(0xffffffffu, max(v0, v1)), min(v0 - 1u, v1 - 1u), u == 0);
+      const float lift = pow2(267 - units.unit);           // 2^14 over the power of two above the scale
+      const float falls = units.wide ? (float)d : 0.f;
+      float most[NB][2], neg[NB][2], corr[NB][2];
+      bool moved = d != 0;
+#pragma unroll
+      for (int m = 0; m < NB; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) most[m][r] = m_run[m][r] - falls;
+      if (__builtin_expect(!units.wide, 1)) {
+#pragma unroll
+        for (int i = 0; i < NM; ++i)
+#pragma unroll
+          for (int m = 0; m < NB; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) most[m][r] = max3(most[m][r], sacc[m][i][r], sacc[m][i][2 + r]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NM; ++i) {
+          const float a0 = attq::counts(vs[16 * i + g] * lift * 0x1p-14f), a1 = attq::counts(vs[16 * i + g + 8] * lift * 0x1p-14f);
+#pragma unroll
+          for (int m = 0; m < NB; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) most[m][r] = max3(most[m][r], sacc[m][i][r] + a0, sacc[m][i][2 + r] + a1);
+        }
+      }
 #pragma unroll
       for (int m = 0; m < NB; ++m)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float mx = m_run[m][r];
-#pragma unroll
-          for (int i = 0; i < NM; ++i) mx = max3(mx, sacc[m][i][r], sacc[m][i][2 + r]);
+          const float before = m_run[m][r] - falls;
+          float mx = most[m][r];
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
           const float ref = mx == -INFINITY ? 0.f : mx;
-          corr[m][r] = ex2_approx(m_run[m][r] - ref);
-          moved = moved || mx != m_run[m][r];
+          corr[m][r] = ex2_approx(before - ref);
+          moved = moved || mx != before;
           m_run[m][r] = mx;
           neg[m][r] = -ref;
         }
       if (__any_sync(0xffffffffu, moved)) {
+        const float step = units.wide ? 1.f : attq::step_of(d), step_l = units.wide ? pow2(127 + d) : 1.f;
 #pragma unroll
         for (int m = 0; m < NB; ++m) {
           mul2(l_run[m][0], l_run[m][1], corr[m][0], corr[m][1]);
+          mul2(l_run[m][0], l_run[m][1], step_l, step_l);
           mul2(corr[m][0], corr[m][1], step, step);
 #pragma unroll
           for (int c = 0; c < C::CHUNKS; ++c) {
@@ -399,12 +420,10 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
       l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 8);
       l_run[m][r] += __shfl_xor_sync(0xffffffffu, l_run[m][r], 16);
     }
-  const float unlift = pow2(e_run - 13);
   auto row_out = [&](int row) {                            // of the item's rows
     const int token = row / G;
     return o + (((size_t)b * n + token) * heads + h * G + row - token * G) * DH;
   };
-  auto inverse = [](float l) { return l > 0.f ? 1.0f / l : l; };   // no key: zeros; NaN stays
   const int n_parts = sp.cs * sp.nk;
   if (n_parts == 1) {
     if (active && ok) {
@@ -415,15 +434,16 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
           const int row = row_w + 8 * m + 2 * t + r;
           if (row < R) {
             uint16_t* to = row_out(row) + 2 * g;
-            const float f = inverse(l_run[m][r]) * unlift;
+            const float2 f = attq::unit_over(l_run[m][r], units.unit - 13);
 #pragma unroll
-            for (int c = 0; c < C::CHUNKS; ++c) *reinterpret_cast<uint32_t*>(to + 16 * c) = pack_a16x2(oacc[m][c][r] * f, oacc[m][c][2 + r] * f, o_bf16 != 0);
+            for (int c = 0; c < C::CHUNKS; ++c)
+              *reinterpret_cast<uint32_t*>(to + 16 * c) = pack_a16x2(oacc[m][c][r] * f.x * f.y, oacc[m][c][2 + r] * f.x * f.y, o_bf16 != 0);
           }
         }
     }
     return;
   }
-  // ---- partial results to the owners of the rows, then the merge
+  // ---- partial results, means of values already (their sums could leave the format), to the owners of the rows, then the merge
   const int rows_cta = sp.nr * RPW, own = (rows_cta + sp.cs - 1) / sp.cs;
   if (sp.cs > 1) {
     __syncwarp();
@@ -439,12 +459,19 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
         if (row_block + in < R) {
           uint32_t dst = recv + 4u * (uint32_t)(((rank * sp.nk + wk) * own + in - owner * own) * C::ROW);
           if (sp.cs > 1) dst = ptx::mapa(dst, (uint32_t)owner);
+          const float2 f = attq::unit_over(l_run[m][r], units.unit - 13);
 #pragma unroll
           for (int c = 0; c < C::CHUNKS; ++c)
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * (16 * c + 2 * g)), "f"(oacc[m][c][r] * unlift),
-                         "f"(oacc[m][c][2 + r] * unlift) : "memory");
-          if (g == 0)
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * DH), "f"(m_run[m][r]), "f"(l_run[m][r]) : "memory");
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * (16 * c + 2 * g)), "f"(oacc[m][c][r] * f.x * f.y),
+                         "f"(oacc[m][c][2 + r] * f.x * f.y) : "memory");
+          if (g == 0) {
+            float ref = m_run[m][r], l = l_run[m][r];
+            if (__builtin_expect(units.wide, 0) && l > 0.f) {                   // (references and sums far from the logits: the power of two belongs to the reference)
+              ref += (float)((int)(__float_as_uint(l) >> 23) - 127);
+              l = __int_as_float((__float_as_int(l) & 0x7fffff) | 0x3f800000);
+            }
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst + 4u * DH), "f"(ref), "f"(l * 0x1p-24f) : "memory");   // (below 1: no sum leaves the format)
+          }
         }
       }
   }
@@ -465,13 +492,13 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
     for (int s = 0; s < n_parts; ++s) mx = fmaxf(mx, p[s * stride + DH]);
     if (mx == -INFINITY) mx = 0.f;
     for (int s = 0; s < n_parts; ++s) {
-      const float w = ex2_approx(p[s * stride + DH] - mx);
+      const float w = ex2_approx(p[s * stride + DH] - mx) * p[s * stride + DH + 1];
       const float4 v = *reinterpret_cast<const float4*>(p + s * stride + c);
-      l = fmaf(w, p[s * stride + DH + 1], l);
+      l += w;
       acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y);
       acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
     }
-    const float f = inverse(l);
+    const float f = l > 0.f ? 1.0f / l : l;                // (no key: zeros; NaN stays)
     uint2 v;
     v.x = pack_a16x2(acc.x * f, acc.y * f, o_bf16 != 0);
     v.y = pack_a16x2(acc.z * f, acc.w * f, o_bf16 != 0);

@@ -19,6 +19,7 @@
 // All waits are bounded and report through the status word.
 #include <cuda.h>
 
+#include "attention_quantized.cuh"
 #include "kernels.h"
 #include "launch_pdl.h"
 #include "sm100_ptx.cuh"
@@ -28,6 +29,8 @@ namespace marche {
 
 namespace {
 
+using attq::pow2;
+
 constexpr int QT = 128;                    // rows of a unit (= TMEM lanes)
 constexpr int KT = 64;                     // keys per tile
 constexpr int NSTG = 3, NB2 = 2, NSC = 4;  // staging slots; operand tiles of K and of V; slots of scales (a converter is at most three tiles ahead of a softmax)
@@ -35,7 +38,9 @@ enum { ST_ATT_QUANTIZED_TC = 0x53 };
 // barriers of one stream
 enum { B_STG_FULL = 0, B_STG_EMPTY = B_STG_FULL + NSTG, B_K_FULL = B_STG_EMPTY + NSTG, B_K_EMPTY = B_K_FULL + NB2, B_V_FULL = B_K_EMPTY + NB2,
        B_V_EMPTY = B_V_FULL + NB2, B_SC_FULL = B_V_EMPTY + NB2, B_Q_FULL = B_SC_FULL + NSC, B_TOP, B_Q_EMPTY, B_S_FULL, B_S_FREE, B_P_FULL, B_O_FULL, NB };
-constexpr int kScaleSlot = 2 * KT + 4;     // words: ks in units of log2 [64], vs lifted [64], step, unlift, 1 + buffer of the rows' own factors (0: none)
+constexpr int kScaleSlot = 2 * KT + 4;     // words: ks in units of log2 [64], vs lifted [64], step, unlift, flags, by how much a wide sample's unit rises
+enum { F_BUFFER = 1, F_OWN = 2, F_WIDE = 4 };   // which buffer of the rows' own factors, where they have some; value scales far apart
+constexpr int kSpread = 10;                // a row's largest product is at least 2^(7 - 1 - 10) before its sample counts as wide
 
 template <int DH, int NS> struct Cfg {
   static constexpr int NC = 2;                             // converters of a stream
@@ -129,7 +134,6 @@ template <uint32_t SEL> MARCHE_DEVINL uint32_t two_of(uint32_t biased) {
 MARCHE_DEVINL void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-MARCHE_DEVINL float pow2(int biased_exponent) { return __int_as_float(biased_exponent << 23); }
 
 // Byte offset of 16-byte piece c of key r in a staging tile, as TMA wrote it (64- and 128-byte rows swizzled, 80-byte rows as they are): eight
 // consecutive keys' pieces lie on different banks.
@@ -409,7 +413,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
       __syncwarp();
       arrive(B_Q_FULL);
       ++qn;
-      int e_run = 14;                                      // biased exponent above every value scale of the unit so far
+      attq::Units units;
       for (int kt = 0; kt < un.n_kv; ++kt) {
         if (!wait(B_STG_FULL + stg, stg_phase)) { ok = false; break; }
         const int key = part * 32 + lane;
@@ -440,17 +444,18 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         const int left = un.len - kt * KT;               // keys of this tile that count (behind them scales may be anything)
         const float ks = key < left ? raw_s[key] : 0.f, vs = key < left ? raw_s[KT + key] : 0.f;
         const uint32_t other = (key ^ 32) < left ? __float_as_uint(raw_s[KT + (key ^ 32)]) : 0u;
-        const int e_new = max(e_run, min((int)(__reduce_max_sync(0xffffffffu, max(__float_as_uint(vs), other)) >> 23), 254));   // (not negative: they order as integers)
+        const uint32_t mine = __float_as_uint(vs);
+        const int d = units.take<kSpread>(__reduce_max_sync(0xffffffffu, max(mine, other)), min(mine - 1u, other - 1u), kt == 0);
         if (!wait(B_K_EMPTY + slot, phase)) { ok = false; break; }
         scale_slot[key] = ks * c_log2;
-        scale_slot[KT + key] = vs * pow2(260 - e_new);   // below 2^7, so that weights of up to 2^8 stay below fp16's end
+        scale_slot[KT + key] = vs * pow2(260 - units.unit);   // below 2^7, so that weights of up to 2^8 stay below fp16's end
         if (part == 0 && lane == 0) {
-          scale_slot[2 * KT] = e_new == e_run || kt == 0 ? 1.f : (e_new - e_run > 120 ? 0.f : pow2(127 - (e_new - e_run)));
-          scale_slot[2 * KT + 1] = pow2(e_new - 6);
+          scale_slot[2 * KT] = units.wide ? 1.f : attq::step_of(d);
+          scale_slot[2 * KT + 1] = pow2(units.unit - 6);
           // (two buffers: who writes a row's factor for the unit after next has seen this unit's S taken out of tensor memory)
-          scale_slot[2 * KT + 2] = __int_as_float(own ? 1 + ((qn - 1) & 1) : 0);
+          scale_slot[2 * KT + 2] = __int_as_float((units.wide ? F_WIDE : 0) | (own ? F_OWN | ((qn - 1) & 1) : 0));
+          scale_slot[2 * KT + 3] = units.wide ? (float)d : 0.f;
         }
-        e_run = e_new;
         __syncwarp();
         arrive(B_SC_FULL + sc);
         if (++sc == NSC) sc = 0;
@@ -495,15 +500,15 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         const float4* vs4 = ks4 + KT / 4;
         const float4 of_tile = ks4[KT / 2];
         const float step = of_tile.x;
-        const int own = __float_as_int(of_tile.z);
+        const int flags = __float_as_int(of_tile.z);
         unlift = of_tile.y;
         if (++sc == NSC) { sc = 0; sc_phase ^= 1u; }
         const int lim = un.len - i * KT;                   // keys of this tile that exist
         // The previous P V of this unit has read its weights and added to O.  (Without it no warp may announce this tile's weights.)
         auto previous_done = [&]() { return i == 0 || wait(B_O_FULL, (uint32_t)(t - 1) & 1u); };
         if (warp_valid) {
-          if (own) {                                       // (in place, so that units that need none of it pay a branch)
-            const float power = *(reinterpret_cast<const float*>(gen + C::OFF_FACTOR) + (2 * j + own - 1) * QT + r);
+          if (__builtin_expect(flags & F_OWN, 0)) {                             // (in place, so that units that need none of it pay a branch)
+            const float power = *(reinterpret_cast<const float*>(gen + C::OFF_FACTOR) + (2 * j + (flags & F_BUFFER)) * QT + r);
 #pragma unroll 1
             for (int qc = 0; qc < KT / 16; ++qc) scale_in_place(t_s + (uint32_t)(qc * 16), power);
             tmem_st_wait();
@@ -542,16 +547,27 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
           };
           logits(sa, ks4, mx[0], mx[1], lim);
           logits(sb, ks4 + KT / 8, mx[2], mx[3], lim - KT / 2);
-          const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), falls = 0.f;
+          if (__builtin_expect(flags & F_WIDE, 0)) {                            // what counts for the reference; the reference falls by as much as the unit rises
+            tmax = -INFINITY;
+            falls = of_tile.w;
+#pragma unroll
+            for (int c = 0; c < KT / 2; ++c) {
+              const float* vs = reinterpret_cast<const float*>(vs4);
+              tmax = max3(tmax, sa[c] + attq::counts(vs[c] * 0x1p-7f), sb[c] + attq::counts(vs[KT / 2 + c] * 0x1p-7f));
+            }
+            tmax += falls;
+          }
           // lazy reference: it moves only when this tile exceeds it by more than 2^8 (and to the first tile's maximum)
           const bool move = i == 0 || tmax > 8.0f;
-          const bool any_move = __any_sync(0xffffffffu, move), rescale = i > 0 && (step != 1.f || any_move);
-          float f = 1.0f;
+          const bool any_move = __any_sync(0xffffffffu, move || falls != 0.f), rescale = i > 0 && (step != 1.f || any_move);
+          float f = 1.0f, f_l = 1.0f;
           if (any_move) {
             const float d = move ? tmax : 0.f;
-            m_ref += d;
             f = i > 0 ? ex2_approx(-d) : 0.f;
-            const float2 dd = make_float2(-d, -d);
+            f_l = f * ex2_approx(falls);
+            m_ref += d - falls;
+            const float2 dd = make_float2(falls - d, falls - d);
 #pragma unroll
             for (int c = 0; c < KT / 2; c += 2) {
               const float2 x = __fadd2_rn(make_float2(sa[c], sa[c + 1]), dd), y = __fadd2_rn(make_float2(sb[c], sb[c + 1]), dd);
@@ -585,7 +601,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
 #pragma unroll 1
             for (int qc = 0; qc < DH / 16; ++qc) scale_in_place(t_o + (uint32_t)(qc * 16), fo);
           }
-          l = fmaf(l, f, (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
+          l = fmaf(l, f_l, (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y));
           tmem_st_wait();
         } else {
           if (lane == 0) ptx::mbar_arrive(bar(j, B_S_FREE));
@@ -601,7 +617,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
       if (!wait(B_O_FULL, (uint32_t)(t - 1) & 1u)) { ok = false; break; }
       ptx::tc_fence_after();
       if (warp_valid) {
-        const float inv = unlift / l;
+        const float2 inv = attq::unit_over(l, (int)(__float_as_uint(unlift) >> 23));
 #pragma unroll
         for (int qc = 0; qc < DH / 16; ++qc) {
           uint32_t ov[16];
@@ -610,7 +626,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
           if (there) {
             uint32_t w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = pack_a16x2(__uint_as_float(ov[2 * e]) * inv, __uint_as_float(ov[2 * e + 1]) * inv, o_bf16 != 0);
+            for (int e = 0; e < 8; ++e) w[e] = pack_a16x2(__uint_as_float(ov[2 * e]) * inv.x * inv.y, __uint_as_float(ov[2 * e + 1]) * inv.x * inv.y, o_bf16 != 0);
             reinterpret_cast<uint4*>(dst)[2 * qc] = make_uint4(w[0], w[1], w[2], w[3]);
             reinterpret_cast<uint4*>(dst)[2 * qc + 1] = make_uint4(w[4], w[5], w[6], w[7]);
           }

@@ -732,3 +732,62 @@ def test_keys_at_the_upper_end_of_the_range(models, both_kernels):
     for n in (3, 140):
         q = (randn(gen, B * n, H * dh) * 2.0 ** -121).to(torch.bfloat16)
         assert_attention(attend(m, cache, q, H * dh, n, H, None), cache, q, n, H, None)
+
+
+def outlier_reference(cache, q, n, heads, kv_len):
+    """o, A and S 127 max(p vs) of the row itself: what its smallest steps are relative to."""
+    o, A, _ = reference(cache, q, n, heads, kv_len)
+    B, S, Hkv, dh = cache.B, cache.S, cache.n_kv_heads, cache.head_dim
+    k, vs = values(cache)[0], cache.scales[1, :, :, :S].double()
+    x = torch.einsum("bnhd,bshd->bnhs", q.double().view(B, n, heads, dh), k.repeat_interleave(heads // Hkv, 2)) / dh ** 0.5
+    if kv_len is not None:
+        x = x.masked_fill(torch.arange(S, device="cuda") >= kv_len.view(B, 1, 1, 1), float("-inf"))
+    p = torch.softmax(x, -1).nan_to_num(0.0)
+    top = (p * vs.repeat_interleave(heads // Hkv, 1).unsqueeze(1).nan_to_num(0.0)).amax(-1)
+    return o, A, (S * 127 * top).view(B * n, heads, 1)
+
+
+@pytest.mark.parametrize("operand", ["f16", "bf16"])
+@pytest.mark.parametrize("dh,heads,kv_heads,n", [(64, 2, 2, 1), (64, 4, 1, 30), (80, 2, 2, 140), (128, 2, 2, 20), (128, 4, 4, 150)])
+@pytest.mark.parametrize("power,logit", [(20, -25.0), (45, -25.0), (60, -60.0), (100, -60.0), (119, -200.0), (-60, 30.0)])
+@pytest.mark.parametrize("where", ["first", "middle", "last", "tile", "all but few"])
+def test_a_value_without_weight_does_not_push_the_others_out(models, both_kernels, where, power, logit, dh, heads, kv_heads, n, operand):
+    """Keys whose value scale lies far above (below) the others' at a weight of next to nothing (of nearly all).  A weight is off by half a step of
+    2^-24 at most, and the row's largest product of weight and value scale is kept at 2^-4 or above: S 2^-21 127 max(p vs) bounds what
+    the steps of small weights do; else the bounds of all tests here."""
+    m, gen, B, S = models[operand], gen_of(n + dh), 2, 700
+    cache = filled_cache(m, gen, B, S, kv_heads, dh, spread=False)
+    keys = {"first": slice(0, 1), "middle": slice(330, 332), "last": slice(S - 1, S), "tile": slice(0, 64), "all but few": slice(5, 690)}[where]
+    ones = cache.codes[0].view(B, S, kv_heads, dh)
+    ones[:, keys] = 0
+    ones[:, keys, :, 0] = 127 if logit > 0 else -127                 # k = -+ that, 0, 0, ..: q's first value is 8
+    cache.scales[0, :, :, keys] = abs(logit) * dh ** 0.5 / 8 / 127
+    cache.scales[1, :, :, keys] *= 2.0 ** power
+    if where != "all but few":
+        cache.scales[1, 1, :, keys] *= 2.0 ** -7                      # (samples differ)
+    q = randn(gen, B * n, heads, dh)
+    q[:, :, 0] = 8
+    q = q.to(torch.bfloat16).view(B * n, heads * dh)
+    for kv_len in (None, torch.tensor([S - 3, 340], dtype=torch.int32, device="cuda")):
+        o = attend(m, cache, q, heads * dh, n, heads, kv_len)
+        want, A, low = outlier_reference(cache, q, n, heads, kv_len)
+        # sums of |q k| reach 2^11 beside the keys of the given logit: off by 2^11 2^-22 sqrt(1 / dh); a value beyond the type's end is not asked for
+        limit = (2.0 ** -11 + 2.0 ** -10) * A + 2.0 ** -21 * low + HALF[o.dtype] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -24
+        fits = want.abs() < 6e4
+        assert bool(((o.double().view_as(want) - want).abs() <= limit)[fits].all())
+        assert torch.equal(o, attend(m, cache, q, heads * dh, n, heads, kv_len)) or not bool(fits.all())
+
+
+def test_values_far_apart_in_some_samples_only(models, both_kernels):
+    """More units than SMs: what a unit met does not follow into the next one."""
+    m, gen, B, S, H, dh, n = models["f16"], gen_of(8), 120, 200, 4, 64, 150
+    cache = filled_cache(m, gen, B, S, H, dh)
+    q = randn(gen, B * n, H * dh).to(torch.bfloat16)
+    want = attend(m, cache, q, H * dh, n, H, None)
+    cache.scales[1, ::3, 1, 7] *= 2.0 ** 60
+    cache.scales[1, 1::3, :, 100:] *= 2.0 ** -50
+    o = attend(m, cache, q, H * dh, n, H, None).view(B, n, H, dh)
+    assert torch.equal(o[2::3], want.view_as(o)[2::3]) and torch.equal(o[::3, :, [0, 2, 3]], want.view_as(o)[::3, :, [0, 2, 3]])
+    for b in (1, 4, 58, 118):
+        part = QuantizedCache(cache.codes[:, b:b + 1].contiguous(), cache.scales[:, b:b + 1].contiguous(), H)
+        assert_attention(o[b], part, q[b * n:(b + 1) * n], n, H, None)
