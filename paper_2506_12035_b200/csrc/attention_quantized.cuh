@@ -29,6 +29,23 @@ MARCHE_DEVINL float lg2_approx(float x) {
   return y;
 }
 
+// Magnitudes of two 16-bit numbers at once: the larger ones, and the smaller ones that are not 0, less 1.
+MARCHE_DEVINL uint32_t larger2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+MARCHE_DEVINL uint32_t smaller2_less_1(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("{\n.reg .b32 t;\nadd.u16x2 t, %2, %3;\nmin.u16x2 %0, %1, t;\n}" : "=r"(r) : "r"(a), "r"(b), "r"(0xffffffffu));
+  return r;
+}
+// Of both halves of a word the larger one that is a finite bf16 number's magnitude, or 0.
+MARCHE_DEVINL uint32_t finite_of(uint32_t w) {
+  const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+  return max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u);
+}
+
 // The largest value scale so far and the unit, as biased exponents, and a lane's smallest scale so far that is not 0.
 struct Units {
   int top = 14, unit = 14;                                 // (14: the lowest whose factors exist)

@@ -203,11 +203,14 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
     const float scale_log2 = rsqrtf((float)DH) * 1.4426950408889634f;
 #pragma unroll
     for (int m = 0; m < NB; ++m) {
-      uint32_t top = 0;
+      uint32_t both = 0;
 #pragma unroll
-      for (int s = 0; s < C::STEPS; ++s) {
-        const uint32_t big = max(max(x[m][s].x & 0x7fffu, (x[m][s].x >> 16) & 0x7fffu), max(x[m][s].y & 0x7fffu, (x[m][s].y >> 16) & 0x7fffu));
-        top = max(top, big < 0x7f80u ? big : 0u);          // (infinities and NaN stay what they are)
+      for (int s = 0; s < C::STEPS; ++s) both = attq::larger2(both, attq::larger2(x[m][s].x & 0x7fff7fffu, x[m][s].y & 0x7fff7fffu));
+      uint32_t top = max(both & 0xffffu, both >> 16);
+      if (top >= 0x7f80u) {                                // (infinities and NaN stay what they are)
+        top = 0;
+#pragma unroll
+        for (int s = 0; s < C::STEPS; ++s) top = max(top, max(attq::finite_of(x[m][s].x), attq::finite_of(x[m][s].y)));
       }
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));   // of row g

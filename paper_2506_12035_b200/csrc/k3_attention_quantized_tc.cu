@@ -344,7 +344,7 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
       {
         constexpr int ROWS = QT / NC / 32;                 // of a lane
         uint4 x[ROWS][DH / 8];
-        uint32_t top[ROWS], low = 0xffffffffu;             // largest finite one of each row; smallest of all that are not 0, less 1
+        uint32_t top[ROWS], low = 0xffffffffu;             // largest finite one of each row; smallest of all that are not 0, less 1 (0xffff: none)
 #pragma unroll
         for (int p = 0; p < ROWS; ++p) {
           const int row = un.row0 + part * (QT / NC) + p * 32 + lane, token = row / sh.G;
@@ -355,18 +355,25 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         }
 #pragma unroll
         for (int p = 0; p < ROWS; ++p) {
-          top[p] = 0;
+          uint32_t both = 0;
 #pragma unroll
           for (int c = 0; c < DH / 8; ++c) {
             const uint32_t w[4] = {x[p][c].x, x[p][c].y, x[p][c].z, x[p][c].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                  // (infinities and NaN stay what they are, in their row)
-              const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;
-              top[p] = max(top[p], max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-              low = min(low, min(lo - 1u, hi - 1u));
+            for (int i = 0; i < 4; ++i) {
+              both = attq::larger2(both, w[i] & 0x7fff7fffu);
+              low = attq::smaller2_less_1(low, w[i] & 0x7fff7fffu);
             }
           }
+          top[p] = max(both & 0xffffu, both >> 16);
+          if (top[p] >= 0x7f80u) {                         // (infinities and NaN stay what they are, in their row)
+            top[p] = 0;
+#pragma unroll
+            for (int c = 0; c < DH / 8; ++c)
+              top[p] = max(max(top[p], max(attq::finite_of(x[p][c].x), attq::finite_of(x[p][c].y))), max(attq::finite_of(x[p][c].z), attq::finite_of(x[p][c].w)));
+          }
         }
+        low = min(low & 0xffffu, low >> 16);
         uint32_t all = top[0];
 #pragma unroll
         for (int p = 1; p < ROWS; ++p) all = max(all, top[p]);

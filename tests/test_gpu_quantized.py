@@ -791,3 +791,19 @@ def test_values_far_apart_in_some_samples_only(models, both_kernels):
     for b in (1, 4, 58, 118):
         part = QuantizedCache(cache.codes[:, b:b + 1].contiguous(), cache.scales[:, b:b + 1].contiguous(), H)
         assert_attention(o[b], part, q[b * n:(b + 1) * n], n, H, None)
+
+
+def test_rows_with_infinities_beside_ordinary_ones(models, both_kernels):
+    """A row that holds an infinity or a NaN has no numbers in its result; the rows beside it keep theirs."""
+    m, gen, B, S, H, dh, n = models["f16"], gen_of(15), 2, 150, 2, 80, 37
+    cache = filled_cache(m, gen, B, S, H, dh)
+    q = randn(gen, B * n, H, dh).to(torch.bfloat16)
+    want = attend(m, cache, q.view(B * n, -1), H * dh, n, H, None).view(B * n, H, dh)
+    bad = q.clone()
+    bad[3, 0, 7], bad[5, 1, 79], bad[40, 1, 0], bad[40, 1, 1] = float("inf"), float("nan"), float("-inf"), 1e30
+    o = attend(m, cache, bad.view(B * n, -1), H * dh, n, H, None).view(B * n, H, dh)
+    rest = torch.ones(B * n, H, dtype=torch.bool, device="cuda")
+    for row, head in ((3, 0), (5, 1), (40, 1)):
+        assert bool(o[row, head].isnan().all())
+        rest[row, head] = False
+    assert torch.equal(o[rest], want[rest])
