@@ -445,9 +445,9 @@ int marche_attention_two_segment(marche_ctx* ctx, const void* qkv, int ld, int n
  *   codes   int8  [2][batch][seq_len][n_kv_heads * head_dim]   ([0] holds K, [1] V; -127 .. 127)
  *   scales  float [2][batch][n_kv_heads][pad], pad = seq_len rounded up to a multiple of 64; the entries
  *           behind seq_len are neither read for their values nor written
- * head_dim 64, 80 or 128 and seq_len up to MARCHE_QUANTIZED_MAX_SEQ (MARCHE_ESHAPE otherwise); both arrays
- * 16-byte aligned device memory of the caller, of the sizes that the two functions return (0 for
- * dimensions that are not supported). */
+ * head_dim 64, 80 or 128, seq_len up to MARCHE_QUANTIZED_MAX_SEQ and batch * n_kv_heads * head_dim below 2^30
+ * (MARCHE_ESHAPE otherwise); both arrays 16-byte aligned device memory of the caller, of the sizes that the two
+ * functions return (0 for dimensions that are not supported). */
 #define MARCHE_QUANTIZED_MAX_SEQ (1 << 24)
 typedef struct {
   int8_t* codes;
@@ -487,13 +487,15 @@ int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, 
                                const marche_quantized_cache* cache, const int32_t* kv_len, void* o, marche_stream stream);
 
 /* A weight matrix [n][k] (outputs, inputs) of 4 bits: w = code * scale, code -8 .. 7, one bf16 scale per output and
- * `group` neighbouring inputs.  n % 16 == 0, k % 64 == 0, group 32, 64 or 128, k % group == 0 (MARCHE_ESHAPE).
+ * `group` neighbouring inputs.  n % 16 == 0, k % 64 == 0 up to MARCHE_QUANTIZED_MAX_K, group 32, 64 or 128, k % group == 0
+ * (MARCHE_ESHAPE).
  *   codes   the size that marche_quantized_weights_bytes returns (0: not supported), in the order in which the kernel
  *           multiplies: [n/16][k/64][lane 0..31][word 0..3], little-endian words of eight nibbles code + 8.
  *           With g = lane / 4, t = lane % 4, nibble i of word s (i = r + 4 e, r = 0..3, e = 0, 1; bits 4 r + 16 e up)
  *           holds output 16 tile + g + 8 (r % 2), input 64 chunk + 32 (s / 2) + 8 t + 4 (s % 2) + 2 (r / 2) + e.
  *   scales  bf16 [n/16][k/group][16], outputs 0, 8, 1, 9, .. 7, 15 of a tile; *scales_bytes receives their size
  * Both 16-byte aligned. */
+#define MARCHE_QUANTIZED_MAX_K (64 * 65535)
 typedef struct {
   void* codes;
   void* scales;

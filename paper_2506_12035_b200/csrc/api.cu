@@ -851,18 +851,17 @@ namespace {
 constexpr int kScalePad = 64;
 
 bool quantized_shape(int batch, int seq_len, int n_kv_heads, int head_dim) {
-  return batch >= 1 && seq_len >= 1 && n_kv_heads >= 1 && (head_dim == 64 || head_dim == 80 || head_dim == 128);
+  return batch >= 1 && seq_len >= 1 && seq_len <= MARCHE_QUANTIZED_MAX_SEQ && n_kv_heads >= 1 && (head_dim == 64 || head_dim == 80 || head_dim == 128) &&
+         (int64_t)batch * n_kv_heads <= INT32_MAX / 2 / head_dim;
 }
 
-inline int scale_pad(int seq_len) { return (int)(((int64_t)seq_len + kScalePad - 1) / kScalePad * kScalePad); }
+inline int scale_pad(int seq_len) { return (seq_len + kScalePad - 1) / kScalePad * kScalePad; }   // (of a supported one)
 
 // Checks a caller's cache; what the kernels take of it.
 int quantized_cache(marche_ctx* ctx, const marche_quantized_cache* cache, QuantizedKv* kv) {
   if (!cache || !cache->codes || !cache->scales) return MARCHE_EINVAL;
   if (cache->batch < 1 || cache->seq_len < 1 || cache->n_kv_heads < 1) return MARCHE_EINVAL;
-  if (!quantized_shape(cache->batch, cache->seq_len, cache->n_kv_heads, cache->head_dim) || cache->seq_len > MARCHE_QUANTIZED_MAX_SEQ ||
-      (int64_t)cache->batch * cache->n_kv_heads * cache->head_dim > INT32_MAX / 2)
-    return MARCHE_ESHAPE;
+  if (!quantized_shape(cache->batch, cache->seq_len, cache->n_kv_heads, cache->head_dim)) return MARCHE_ESHAPE;
   if (((uintptr_t)cache->codes | (uintptr_t)cache->scales) & 15) return misaligned(ctx, "8-bit cache");
   *kv = {cache->codes, cache->scales, cache->batch, cache->seq_len, cache->n_kv_heads, cache->head_dim, scale_pad(cache->seq_len)};
   return MARCHE_OK;
@@ -941,14 +940,14 @@ int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, 
 }
 
 size_t marche_quantized_weights_bytes(int n, int k, int group, size_t* scales_bytes) {
-  const bool ok = n >= 16 && k >= 64 && n % 16 == 0 && k % 64 == 0 && (group == 32 || group == 64 || group == 128) && k % group == 0;
+  const bool ok = n >= 16 && k >= 64 && n % 16 == 0 && k % 64 == 0 && k <= MARCHE_QUANTIZED_MAX_K && (group == 32 || group == 64 || group == 128) && k % group == 0;
   if (scales_bytes) *scales_bytes = ok ? (size_t)n * (k / group) * 2 : 0;
   return ok ? (size_t)n * k / 2 : 0;
 }
 
 int marche_quantize_weights(marche_ctx* ctx, const float* w, const marche_quantized_weights* out, marche_stream stream) {
   if (!ctx || !w || !out || !out->codes || !out->scales || out->n < 1 || out->k < 1 || out->group < 1) return MARCHE_EINVAL;
-  if (!ctx->bf16 || !marche_quantized_weights_bytes(out->n, out->k, out->group, nullptr) || out->k / 64 > 65535) return MARCHE_ESHAPE;
+  if (!ctx->bf16 || !marche_quantized_weights_bytes(out->n, out->k, out->group, nullptr)) return MARCHE_ESHAPE;
   MARCHE_ENTER(ctx);
   if (((uintptr_t)w | (uintptr_t)out->codes | (uintptr_t)out->scales) & 15) return misaligned(ctx, "weights of 4 bits");
   mark(ctx, MARCHE_KC_OTHER, (cudaStream_t)stream);

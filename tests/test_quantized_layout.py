@@ -125,3 +125,22 @@ def test_pairs_that_hold_tensor_memory_share_no_sm_with_other_clusters(lib):
         for group in (32, 64, 128):
             assert pair(M, group, 1) <= pair(M, group, 2) <= 227 * 1024, (M, group)
             assert pair(M, group, 2) + 1024 + least + 1024 > 228 * 1024, (M, group)
+
+
+@pytest.mark.parametrize("B,S,H,dh", [(1, (1 << 24) + 1, 1, 64), (1, 2 ** 31 - 1, 1, 64), (2, 2 ** 31 - 40, 16, 128), (1 << 24, 1, 1, 64), (1 << 20, 64, 16, 64),
+                                      (2 ** 31 - 1, 1, 2 ** 31 - 1, 128)])
+def test_caches_that_every_call_refuses_have_no_size(lib, B, S, H, dh):
+    from paper_2506_12035_b200 import binding
+    assert lib.marche_quantized_codes_bytes(B, S, H, dh) == 0 and lib.marche_quantized_scales_bytes(B, S, H, dh) == 0
+    with pytest.raises(binding.MarcheError):                         # before anything is allocated
+        binding.Marche.alloc_quantized_cache(type("M", (), {"lib": lib}), B, S, H, dh)
+
+
+def test_largest_caches_have_a_size(lib):
+    assert lib.marche_quantized_scales_bytes(1, 1 << 24, 1, 64) == 8 << 24
+    assert lib.marche_quantized_codes_bytes((1 << 24) - 1, 1, 1, 64) == 128 * ((1 << 24) - 1)
+
+
+@pytest.mark.parametrize("k,ok", [(64 * 65535, True), (64 * 65536, False), (2 ** 31 - 64, False)])
+def test_matrices_that_cannot_be_laid_out_have_no_size(lib, k, ok):
+    assert (lib.marche_quantized_weights_bytes(16, k, 64, None) == 8 * k) is ok and (lib.marche_quantized_weights_bytes(16, k, 64, None) == 0) is not ok
