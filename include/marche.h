@@ -439,7 +439,8 @@ int marche_attention_two_segment(marche_ctx* ctx, const void* qkv, int ld, int n
  * For decoding of few rows, which is bound by the bytes of the cache and of the weight matrices.  The calls
  * stand beside marche_scatter_kv, marche_attention and marche_linear and take their sizes from their own
  * arguments, not from the context's shape; the context gives the element types (16-bit contexts only:
- * MARCHE_ESHAPE in a fp32 one), the device and the status word.  They need no workspace. */
+ * MARCHE_ESHAPE in a fp32 one), the device and the status word.  They need no workspace.
+ * A call of no rows (n or M 0) checks its other arguments, enqueues nothing, and takes NULL for the rows. */
 
 /* One block's K and V, a value being code * scale with one scale per token and cached head:
  *   codes   int8  [2][batch][seq_len][n_kv_heads * head_dim]   ([0] holds K, [1] V; -127 .. 127)

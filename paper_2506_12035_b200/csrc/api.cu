@@ -886,7 +886,7 @@ size_t marche_quantized_scales_bytes(int batch, int seq_len, int n_kv_heads, int
 
 int marche_scatter_kv_quantized(marche_ctx* ctx, const void* k, const void* v, int ld_kv, const int32_t* idx, int n,
                                 const marche_quantized_cache* cache, marche_stream stream) {
-  if (!ctx || !k || !v || n < 0) return MARCHE_EINVAL;
+  if (!ctx || n < 0 || (n && (!k || !v))) return MARCHE_EINVAL;
   if (!ctx->bf16) return MARCHE_ESHAPE;
   MARCHE_ENTER(ctx);
   QuantizedKv kv;
@@ -903,7 +903,7 @@ int marche_scatter_kv_quantized(marche_ctx* ctx, const void* k, const void* v, i
 
 int marche_gather_kv_quantized(marche_ctx* ctx, const marche_quantized_cache* cache, const int32_t* idx, int n, void* k_out,
                                void* v_out, int ld_out, marche_stream stream) {
-  if (!ctx || !k_out || !v_out || n < 0) return MARCHE_EINVAL;
+  if (!ctx || n < 0 || (n && (!k_out || !v_out))) return MARCHE_EINVAL;
   if (!ctx->bf16) return MARCHE_ESHAPE;
   MARCHE_ENTER(ctx);
   QuantizedKv kv;
@@ -920,7 +920,7 @@ int marche_gather_kv_quantized(marche_ctx* ctx, const marche_quantized_cache* ca
 
 int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, int n_heads, const marche_quantized_cache* cache,
                                const int32_t* kv_len, void* o, marche_stream stream) {
-  if (!ctx || !q || !o || n < 0 || n_heads < 1) return MARCHE_EINVAL;
+  if (!ctx || n < 0 || n_heads < 1 || (n && (!q || !o))) return MARCHE_EINVAL;
   if (!ctx->bf16) return MARCHE_ESHAPE;
   MARCHE_ENTER(ctx);
   QuantizedKv kv;
@@ -957,7 +957,7 @@ int marche_quantize_weights(marche_ctx* ctx, const float* w, const marche_quanti
 
 int marche_linear_quantized(marche_ctx* ctx, const void* a, int lda, int M, const marche_quantized_weights* w, const float* bias, int epilogue,
                             void* out, marche_stream stream) {
-  if (!ctx || !a || !w || !w->codes || !w->scales || !bias || !out || M < 0 || w->n < 1 || w->k < 1 || w->group < 1 || lda < w->k) return MARCHE_EINVAL;
+  if (!ctx || M < 0 || (M && (!a || !out)) || !w || !w->codes || !w->scales || !bias || w->n < 1 || w->k < 1 || w->group < 1 || lda < w->k) return MARCHE_EINVAL;
   if (epilogue < 0 || epilogue > 2) return MARCHE_EINVAL;
   if (!ctx->bf16 || !marche_quantized_weights_bytes(w->n, w->k, w->group, nullptr) || M > MARCHE_QUANTIZED_MAX_ROWS) return MARCHE_ESHAPE;
   MARCHE_ENTER(ctx);

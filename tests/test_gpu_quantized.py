@@ -807,3 +807,18 @@ def test_rows_with_infinities_beside_ordinary_ones(models, both_kernels):
         assert bool(o[row, head].isnan().all())
         rest[row, head] = False
     assert torch.equal(o[rest], want[rest])
+
+
+def test_no_rows_at_all(models):
+    """A call without rows enqueues nothing, whatever its empty tensors point to."""
+    m = models["f16"]
+    cache, w = m.alloc_quantized_cache(2, 64, 2, 64), m.quantize_weights(torch.zeros(32, 128, device="cuda"), 64)
+    bf, f16 = torch.empty(0, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 128, dtype=torch.float16, device="cuda")
+    before = m.launch_count()
+    m.scatter_kv_quantized(bf, bf, 128, None, 0, cache)
+    m.scatter_kv_quantized(bf, bf, 128, torch.empty(2, 0, dtype=torch.int32, device="cuda"), 0, cache)
+    m.gather_kv_quantized(cache, None, 0, bf, bf, 128)
+    m.attention_quantized(bf, 128, 0, 2, cache, None, f16)
+    for epi, dtype in enumerate((torch.bfloat16, torch.float32, torch.float16)):
+        m.linear_quantized(f16, w, torch.zeros(32, device="cuda"), epi, torch.empty(0, 32, dtype=dtype, device="cuda"))
+    assert m.launch_count() == before
