@@ -144,6 +144,11 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+def _ptr_on(t: torch.Tensor, device_index: int) -> int:
+    assert t.get_device() == device_index and t.is_contiguous(), "contiguous tensor on the context's device required"
+    return t.data_ptr()
+
+
 # (building a torch.cuda.Stream object costs more than the ctypes call; the short cut is private to torch and may go)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -204,7 +209,7 @@ class QuantizedCache:
         two, B, S, D = codes.shape
         assert codes.is_cuda and codes.is_contiguous() and codes.dtype == torch.int8 and two == 2
         assert n_kv_heads > 0 and D % n_kv_heads == 0
-        assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.float32
+        assert scales.get_device() == codes.get_device() and scales.is_contiguous() and scales.dtype == torch.float32
         assert tuple(scales.shape) == (2, B, n_kv_heads, (S + 63) // 64 * 64), "scales [2][B][kv_heads][S rounded up to 64]"
         self.codes, self.scales = codes, scales
         self.B, self.S, self.n_kv_heads, self.head_dim = B, S, n_kv_heads, D // n_kv_heads
@@ -226,7 +231,7 @@ class QuantizedCache:
         if t is None:
             return None
         assert t.dtype is torch.int32 and t.numel() >= self.B * n, "int32, one entry for every row"
-        return _ptr(t)
+        return _ptr_on(t, self.device_index)
 
 
 class QuantizedWeights:
@@ -234,8 +239,9 @@ class QuantizedWeights:
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, N: int, K: int, group: int):
         assert codes.is_cuda and codes.is_contiguous() and codes.dtype == torch.uint8 and codes.numel() == N * K // 2
-        assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.bfloat16 and scales.numel() == N * (K // group)
-        self.codes, self.scales, self.N, self.K, self.group = codes, scales, N, K, group
+        assert scales.get_device() == codes.get_device() and scales.is_contiguous() and scales.dtype == torch.bfloat16
+        assert scales.numel() == N * (K // group)
+        self.codes, self.scales, self.N, self.K, self.group, self.device_index = codes, scales, N, K, group, codes.get_device()
         self.c = MarcheQuantizedWeights(codes.data_ptr(), scales.data_ptr(), N, K, group)
         self.ref = C.addressof(self.c)
 
@@ -252,6 +258,7 @@ class Marche:
         if not torch.cuda.is_available():
             raise RuntimeError("libmarche needs a CUDA device; there is no CPU path")
         self.lib = load_library()
+        self.device_index = torch.cuda.current_device()
         self.L, self.E, self.D, self.H, self.F, self.S, self.B = L, E, D, H, F, S, B
         self.dtype = dtype
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32      # q/k/v, K/V cache
@@ -441,18 +448,21 @@ class Marche:
         n_scales = self.lib.marche_quantized_scales_bytes(batch, seq_len, n_kv_heads, head_dim)
         if n_codes == 0:
             raise MarcheError(-2)
-        codes = torch.zeros(n_codes, dtype=torch.int8, device="cuda").view(2, batch, seq_len, n_kv_heads * head_dim)
-        scales = torch.zeros(n_scales // 4, dtype=torch.float32, device="cuda").view(2, batch, n_kv_heads, -1)
+        device = torch.device("cuda", self.device_index)
+        codes = torch.zeros(n_codes, dtype=torch.int8, device=device).view(2, batch, seq_len, n_kv_heads * head_dim)
+        scales = torch.zeros(n_scales // 4, dtype=torch.float32, device=device).view(2, batch, n_kv_heads, -1)
         return QuantizedCache(codes, scales, n_kv_heads)
 
     def scatter_kv_quantized(self, k, v, ld_kv, idx, n, cache: QuantizedCache, stream=None):
         """k, v: bf16 rows (or columns of wider rows) with row stride ld_kv; idx int32 [B][n] or None (tokens 0 .. n-1)."""
+        assert cache.device_index == self.device_index, "the cache is on another device than the context"
         cache.check_rows(k, ld_kv, n)
         cache.check_rows(v, ld_kv, n)
         self._check(self.lib.marche_scatter_kv_quantized(self.h, k.data_ptr(), v.data_ptr(), ld_kv, cache.index(idx, n), n, cache.ref,
                                                          _stream(stream)))
 
     def gather_kv_quantized(self, cache: QuantizedCache, idx, n, k_out, v_out, ld_out, stream=None):
+        assert cache.device_index == self.device_index, "the cache is on another device than the context"
         cache.check_rows(k_out, ld_out, n)
         cache.check_rows(v_out, ld_out, n)
         self._check(self.lib.marche_gather_kv_quantized(self.h, cache.ref, cache.index(idx, n), n, k_out.data_ptr(), v_out.data_ptr(),
@@ -460,27 +470,29 @@ class Marche:
 
     def attention_quantized(self, q, ld_q, n, n_heads, cache: QuantizedCache, kv_len, o, stream=None):
         """q: bf16 rows [B*n] (or columns of wider rows) with row stride ld_q; kv_len int32 [B] or None; o dense."""
+        assert cache.device_index == self.device_index, "the cache is on another device than the context"
         cache.check_rows(q, ld_q, n, n_heads * cache.head_dim)
         assert o.dtype == self.operand_dtype and o.numel() >= cache.B * n * n_heads * cache.head_dim
         self._check(self.lib.marche_attention_quantized(self.h, q.data_ptr(), ld_q, n, n_heads, cache.ref, cache.index(kv_len, 1),
-                                                        _ptr(o), _stream(stream)))
+                                                        _ptr_on(o, self.device_index), _stream(stream)))
 
     def quantize_weights(self, w: torch.Tensor, group: int, stream=None) -> QuantizedWeights:
         """w float32 [N][K] -> its layout in 4 bits.  Synchronises, so that it may be used at once."""
-        assert w.dtype == torch.float32
+        assert w.dtype == torch.float32 and w.get_device() == self.device_index
         N, K = w.shape
         n_scales = C.c_size_t(0)
         n_codes = self.lib.marche_quantized_weights_bytes(N, K, group, C.byref(n_scales))
         if n_codes == 0:
             raise MarcheError(-2)
-        q = QuantizedWeights(torch.empty(n_codes, dtype=torch.uint8, device="cuda"),
-                             torch.empty(n_scales.value // 2, dtype=torch.bfloat16, device="cuda"), N, K, group)
+        q = QuantizedWeights(torch.empty(n_codes, dtype=torch.uint8, device=w.device),
+                             torch.empty(n_scales.value // 2, dtype=torch.bfloat16, device=w.device), N, K, group)
         self._check(self.lib.marche_quantize_weights(self.h, _ptr(w), q.ref, _stream(stream)))
         (stream or torch.cuda.current_stream()).synchronize()
         return q
 
     def linear_quantized(self, a, w: QuantizedWeights, bias, epilogue, out, M=None, lda=None, stream=None):
-        assert a.is_cuda and a.dtype == self.operand_dtype and bias.dtype == torch.float32 and bias.numel() >= w.N
+        assert a.get_device() == self.device_index == w.device_index, "rows and weights on the context's device"
+        assert a.dtype == self.operand_dtype and bias.dtype == torch.float32 and bias.numel() >= w.N
         if M is None and lda is None:
             M, lda = a.shape[0], a.stride(0)
             assert a.shape[1] >= w.K and a.stride(1) == 1, "rows of the matrix's inputs"
@@ -488,8 +500,8 @@ class Marche:
             M, lda = a.shape[0] if M is None else M, a.stride(0) if lda is None else lda
             assert M <= 0 or 2 * (a.storage_offset() + (M - 1) * lda + w.K) <= a.untyped_storage().nbytes(), "fewer rows than the call names"
         assert out.dtype == (self.torch_dtype, torch.float32, self.operand_dtype)[epilogue] and out.numel() >= M * w.N
-        self._check(self.lib.marche_linear_quantized(self.h, a.data_ptr(), lda, M, w.ref, _ptr(bias), epilogue, _ptr(out),
-                                                     _stream(stream)))
+        self._check(self.lib.marche_linear_quantized(self.h, a.data_ptr(), lda, M, w.ref, _ptr_on(bias, self.device_index), epilogue,
+                                                     _ptr_on(out, self.device_index), _stream(stream)))
 
     def staging_bytes(self, max_new: int) -> int:
         return self.lib.marche_staging_bytes(self.h, max_new)
