@@ -224,6 +224,7 @@ class QuantizedCache:
         if t.dim() == 2 and t.stride() == (ld, 1) and t.shape[0] >= rows and t.shape[1] >= width:
             return
         if rows > 0:
+            assert t.stride(-1) == 1, "the values of a row lie side by side"
             need = t.storage_offset() + (rows - 1) * ld + width
             assert 2 * need <= t.untyped_storage().nbytes(), "fewer rows than the call names"
 
@@ -493,11 +494,13 @@ class Marche:
     def linear_quantized(self, a, w: QuantizedWeights, bias, epilogue, out, M=None, lda=None, stream=None):
         assert a.get_device() == self.device_index == w.device_index, "rows and weights on the context's device"
         assert a.dtype == self.operand_dtype and bias.dtype == torch.float32 and bias.numel() >= w.N
-        if M is None and lda is None:
-            M, lda = a.shape[0], a.stride(0)
-            assert a.shape[1] >= w.K and a.stride(1) == 1, "rows of the matrix's inputs"
+        assert a.stride(-1) == 1, "the values of a row lie side by side"
+        whole, M = M is None and lda is None, a.shape[0] if M is None else M
+        if lda is None:
+            lda = a.stride(0) if M > 1 else w.K              # (the stride of a single row may be anything)
+        if whole:
+            assert a.shape[1] >= w.K, "rows of the matrix's inputs"
         else:
-            M, lda = a.shape[0] if M is None else M, a.stride(0) if lda is None else lda
             assert M <= 0 or 2 * (a.storage_offset() + (M - 1) * lda + w.K) <= a.untyped_storage().nbytes(), "fewer rows than the call names"
         assert out.dtype == (self.torch_dtype, torch.float32, self.operand_dtype)[epilogue] and out.numel() >= M * w.N
         self._check(self.lib.marche_linear_quantized(self.h, a.data_ptr(), lda, M, w.ref, _ptr_on(bias, self.device_index), epilogue,

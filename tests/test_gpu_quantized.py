@@ -822,3 +822,27 @@ def test_no_rows_at_all(models):
     for epi, dtype in enumerate((torch.bfloat16, torch.float32, torch.float16)):
         m.linear_quantized(f16, w, torch.zeros(32, device="cuda"), epi, torch.empty(0, 32, dtype=dtype, device="cuda"))
     assert m.launch_count() == before
+
+
+def test_rows_as_tensors_come(models):
+    """One row has no stride; rows whose values do not lie side by side are refused."""
+    m, gen, N, K = models["f16"], gen_of(13), 32, 128
+    w = m.quantize_weights(matrix(gen, N, K), 64)
+    codes, scales = unpack(w)
+    a, bias, out = randn(gen, K, 1).to(torch.float16).t(), randn(gen, N), torch.empty(1, N, dtype=torch.bfloat16, device="cuda")
+    assert a.stride(0) < K
+    for kw in ({}, dict(M=1)):
+        out.zero_()
+        m.linear_quantized(a, w, bias, 0, out, **kw)
+        assert_linear(out, a, codes, scales, 64, bias, 0, None)
+    wide, out = randn(gen, 4, 2 * K).to(torch.float16), torch.empty(4, N, dtype=torch.bfloat16, device="cuda")
+    for kw in ({}, dict(M=4), dict(M=4, lda=2 * K)):
+        with pytest.raises(AssertionError):
+            m.linear_quantized(wide[:, ::2], w, bias, 0, out, **kw)
+    cache, rows, o = m.alloc_quantized_cache(1, 64, 2, 64), torch.zeros(4, 512, dtype=torch.bfloat16, device="cuda"), torch.empty(4, 128, dtype=torch.float16, device="cuda")
+    with pytest.raises(AssertionError):
+        m.scatter_kv_quantized(rows[:, ::2], rows[:, ::2], 512, None, 4, cache)
+    with pytest.raises(AssertionError):
+        m.gather_kv_quantized(cache, None, 4, rows[:, ::2], rows[:, ::2], 512)
+    with pytest.raises(AssertionError):
+        m.attention_quantized(rows[:, ::2], 512, 4, 2, cache, None, o)
