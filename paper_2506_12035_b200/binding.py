@@ -236,7 +236,9 @@ class QuantizedCache:
 
 
 class QuantizedWeights:
-    """A weight matrix [N][K] of 4 bits with bf16 scales per group, in marche_quantized_weights' layout."""
+    """A weight matrix [N][K] of 4 bits with bf16 scales per group, in marche_quantized_weights' layout.  Tensors of the caller's own have to be
+    complete in memory before a projection is enqueued (synchronise after writing them, or keep another kernel of the stream in between): it
+    fetches its first codes before the preceding kernel has finished.  What Marche.quantize_weights returns is."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, N: int, K: int, group: int):
         assert codes.is_cuda and codes.is_contiguous() and codes.dtype == torch.uint8 and codes.numel() == N * K // 2
@@ -478,7 +480,8 @@ class Marche:
                                                         _ptr_on(o, self.device_index), _stream(stream)))
 
     def quantize_weights(self, w: torch.Tensor, group: int, stream=None) -> QuantizedWeights:
-        """w float32 [N][K] -> its layout in 4 bits.  Synchronises, so that it may be used at once."""
+        """w float32 [N][K] -> its layout in 4 bits.  A stream given waits for what the current one has enqueued (the memory that the layout
+        gets may have been in use there).  Synchronises, so that the layout may be used at once."""
         assert w.dtype == torch.float32 and w.get_device() == self.device_index
         N, K = w.shape
         n_scales = C.c_size_t(0)
@@ -487,6 +490,8 @@ class Marche:
             raise MarcheError(-2)
         q = QuantizedWeights(torch.empty(n_codes, dtype=torch.uint8, device=w.device),
                              torch.empty(n_scales.value // 2, dtype=torch.bfloat16, device=w.device), N, K, group)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
         self._check(self.lib.marche_quantize_weights(self.h, _ptr(w), q.ref, _stream(stream)))
         (stream or torch.cuda.current_stream()).synchronize()
         return q

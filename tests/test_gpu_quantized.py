@@ -846,3 +846,28 @@ def test_rows_as_tensors_come(models):
         m.gather_kv_quantized(cache, None, 4, rows[:, ::2], rows[:, ::2], 512)
     with pytest.raises(AssertionError):
         m.attention_quantized(rows[:, ::2], 512, 4, 2, cache, None, o)
+
+
+
+def test_weights_laid_out_on_another_stream(models):
+    """Memory that the current stream gave back, but has not finished with, may be what the layout gets."""
+    m, gen, N, K = models["f16"], gen_of(14), 4096, 8192
+    w = matrix(gen, N, K)
+    want = m.quantize_weights(w, 64)
+    codes, scales = want.codes.clone(), want.scales.clone()
+    side = torch.cuda.Stream()
+    del want
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    left = [torch.empty(N * K // 2, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    at = {t.data_ptr() for t in left}
+    left += [torch.empty(N * K // 64, dtype=torch.bfloat16, device="cuda").view(torch.uint8) for _ in range(4)]   # (nothing is to be allocated anew)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    for t in left:
+        t.fill_(255)
+    del left, t
+    got = m.quantize_weights(w, 64, stream=side)
+    torch.cuda.synchronize()
+    assert got.codes.data_ptr() in at
+    assert torch.equal(got.codes, codes) and torch.equal(got.scales, scales)
