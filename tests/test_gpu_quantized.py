@@ -871,3 +871,88 @@ def test_weights_laid_out_on_another_stream(models):
     torch.cuda.synchronize()
     assert got.codes.data_ptr() in at
     assert torch.equal(got.codes, codes) and torch.equal(got.scales, scales)
+
+
+@pytest.mark.parametrize("dh,n", [(64, 1), (80, 30), (128, 3), (64, 140), (128, 150)])
+def test_values_at_the_upper_end_of_the_range(models, both_kernels, dh, n):
+    """V near the largest bf16 number: the mean is one, though the sum over the keys would not be."""
+    m, gen, B, S, H = models["bf16"], gen_of(n + dh), 2, 1500, 2
+    cache = filled_cache(m, gen, B, S, H, dh, spread=False)
+    q = randn(gen, B * n, H * dh).to(torch.bfloat16)
+    cache.scales[1] /= 127 * cache.scales[1, :, :, :S].max()
+    cache.scales[1] *= 2.0 ** 127                                     # (codes of 127 are 2^127)
+    o = attend(m, cache, q, H * dh, n, H, None)
+    want, A, low = reference(cache, q, n, H, None)
+    limit = (2.0 ** -11 + 2.0 ** -13) * A + low + HALF[o.dtype] * want.abs() * (1 + 2.0 ** -10)
+    assert bool(((o.double().view_as(want) - want).abs() <= limit).all())
+
+
+@pytest.mark.parametrize("dh", [64, 80, 128])
+@pytest.mark.parametrize("n,S", [(3, 2), (5, 2), (16, 5), (1, 40)])
+def test_what_the_weights_rounding_left_off(models, dh, n, S):
+    """fp16 outputs of the mma.sync kernel: the rest of a weight is a second operand.  Values that cancel, so that the output's own rounding hides
+    nothing: what is left are logits of |x| < 2^4 (2^-18 of them: 2^-17.5 of a weight with the sum's) and 2^-21 of the weights."""
+    m, gen, B, H = models["f16"], gen_of(n + S + dh), 8, 4
+    m.set_tuning(attention_kernel=KERNELS["mma"])
+    try:
+        cache = filled_cache(m, gen, B, S, H, dh, spread=False)
+        q = (0.5 * randn(gen, B * n, H * dh)).to(torch.bfloat16)
+        p = torch.softmax(torch.einsum("bnhd,bshd->bnhs", q.double().view(B, n, H, dh), values(cache)[0]) / dh ** 0.5, -1)
+        # the second key's values cancel the first one's for the first token's weights, nearly
+        cache.codes[1, :, 0] = 127
+        cache.codes[1, :, 1] = -127
+        cache.scales[1, :, :, 0], cache.scales[1, :, :, 1] = p[:, 0, :, 1].float(), p[:, 0, :, 0].float()
+        o = attend(m, cache, q, H * dh, n, H, None).double().view(B * n, H, dh)
+        want, A, low = reference(cache, q, n, H, None)
+        limit = (2.0 ** -21 + 2.0 ** -17.5) * A + low + HALF[torch.float16] * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -25
+        assert bool(((o - want).abs() <= limit).all()), "error %.3g of the bound" % float(((o - want).abs() / limit).max())
+    finally:
+        m.set_tuning(attention_kernel=binding.ATTENTION_AUTO)
+
+
+# ------------------------------------------------------------------ large matrices, all forms
+LARGE = [  # N, K, group: every kernel for large matrices at every group, pairs with one unit and with several in turn, a single stage of one chunk among them
+    (4864, 4224, 128), (4864, 4224, 64), (4864, 4224, 32), (12288, 2304, 128), (12288, 2304, 64), (12288, 2304, 32), (24576, 1152, 128), (24576, 1152, 64), (24576, 1152, 32),
+    (16384, 1024, 128), (18960, 640, 64), (18960, 640, 32), (151568, 64, 32), (151568, 64, 64), (75792, 128, 128)]
+LARGE_ROWS = [1, 5, 8, 9, 16, 17, 29, 32, 45]
+
+
+@pytest.fixture(scope="module")
+def large_matrix(models):
+    """(N, K, group) -> the matrix laid out, its codes and scales; the last one is kept, since the tests below take them in turn."""
+    last = {}
+
+    def get(N, K, group):
+        if (N, K, group) not in last:
+            last.clear()
+            q = models["f16"].quantize_weights(matrix(gen_of(N + K), N, K), group)
+            last[N, K, group] = (q,) + unpack(q)
+        return last[N, K, group]
+    return get
+
+
+@pytest.mark.parametrize("operand", ["f16", "bf16"])
+@pytest.mark.parametrize("M", LARGE_ROWS)
+@pytest.mark.parametrize("N,K,group", LARGE)
+def test_linear_of_large_matrices_with_all_epilogues(models, large_matrix, operand, N, K, group, M):
+    m, gen = models[operand], gen_of(N + K + M)
+    q, codes, scales = large_matrix(N, K, group)
+    a, bias = randn(gen, M, K + 24).to(TYPES[operand])[:, 8:8 + K], randn(gen, N)
+    for epi in range(3):
+        residual = randn(gen, M, N)
+        out = torch.full((M + 2, N), 7.0, device="cuda", dtype=(torch.bfloat16, torch.float32, TYPES[operand])[epi])
+        if epi == 1:
+            out[:M] = residual
+        m.linear_quantized(a, q, bias, epi, out, M=M, lda=K + 24)
+        assert_linear(out[:M], a, codes, scales, group, bias, epi, residual)
+        assert bool((out[M:] == 7).all())
+
+
+@pytest.mark.parametrize("N,K,group,M", [(768, 768, 64, 1088), (4864, 4224, 128, 500), (2304, 768, 32, 1000), (64, 128, 64, 65536), (9600, 2112, 64, 161)])
+def test_linear_of_many_rows(models, N, K, group, M):
+    m, gen = models["f16"], gen_of(N + M)
+    q = m.quantize_weights(matrix(gen, N, K), group)
+    codes, scales = unpack(q)
+    a, bias, out = randn(gen, M, K).to(torch.float16), randn(gen, N), torch.empty(M, N, dtype=torch.float16, device="cuda")
+    m.linear_quantized(a, q, bias, 2, out)
+    assert_linear(out, a, codes, scales, group, bias, 2, None)

@@ -144,3 +144,27 @@ def test_largest_caches_have_a_size(lib):
 @pytest.mark.parametrize("k,ok", [(64 * 65535, True), (64 * 65536, False), (2 ** 31 - 64, False)])
 def test_matrices_that_cannot_be_laid_out_have_no_size(lib, k, ok):
     assert (lib.marche_quantized_weights_bytes(16, k, 64, None) == 8 * k) is ok and (lib.marche_quantized_weights_bytes(16, k, 64, None) == 0) is not ok
+
+
+def test_large_matrices_of_the_gpu_tests_reach_every_kernel(lib):
+    """Every kernel for large matrices that a projection can get, by rows and group, pairs with more units than there are pairs among them."""
+    from test_gpu_quantized import LARGE, LARGE_ROWS
+    pick = lib._ZN6marche19gemm_quantized_pickEiiii
+    pick.restype, pick.argtypes = GemmShape, [C.c_int] * 4
+    seen = set()
+    for N, K, group in LARGE:
+        for M in LARGE_ROWS:
+            s, rows = pick(M, N, K, group), 16 if M <= 16 else 32
+            if s.tc:
+                units, at_once = -(-N // 128) * -(-M // rows), 148 // s.tc
+                seen.add((s.tc, rows, group, "once" if units <= at_once else "in turn"))
+            elif s.wn:
+                seen.add(("ring", group))
+    for group in (32, 64, 128):
+        assert ("ring", group) in seen
+        for rows in (16, 32):
+            assert (1, rows, group, "once") in seen
+            for turns in ("once", "in turn"):
+                assert (2, rows, group, turns) in seen
+        assert (1, 32, group, "in turn") in seen
+    assert (1, 16, 32, "in turn") in seen and (1, 16, 64, "in turn") in seen
