@@ -10,8 +10,8 @@
 //   2^d, the references fall by d: products over the unit, and with them O, stay as they are, and the sums of weights rise by 2^d.
 // Scales of 16-bit numbers that lie up to 2^125 apart keep to both: a row's largest product is at least 2^-5 of what fp16 holds, and sums of weights
 // stay between 2^-85 and 2^125.
-// Samples that are not wide pay for finding that out (a vote and a running minimum per tile): one token over 4 x 65521 keys at most 88.9 -> 90.5 us,
-// 128 x 43 rows over 320 keys 67.9 -> 68.5, 32 x 1088 rows over 1088 keys within what the compiler's choices move.
+// Samples that are not wide pay for finding that out (a running minimum per tile): one token over 4 x 65521 keys at most 88.9 -> 90.5 us, 128 x 43 rows
+// over 320 keys 65.5 us before and after.  A wide one pays 2 to 4 % in the mma.sync kernel, half again as much in the tcgen05 one (64 logarithms a row and tile).
 #pragma once
 
 #include "common.cuh"
@@ -52,11 +52,16 @@ struct Units {
   uint32_t low = 0xffffffffu;                              // as bits less 1
   bool wide = false;
   // Takes in a tile's largest scale and the smallest that is not 0 of the lane's, less 1 (0xffffffff: none), as bits: scales are not negative, so
-  // they order as integers; NaN counts as the largest number.  All lanes of the warp call; returns by how many powers of two the unit rises.
-  template <int SPREAD> MARCHE_DEVINL int take(uint32_t largest, uint32_t smallest_less_1, bool first) {
+  // they order as integers; NaN counts as the largest number.
+  MARCHE_DEVINL void see(uint32_t largest, uint32_t smallest_less_1) {
     top = max(top, min((int)(largest >> 23), 254));
     low = min(low, smallest_less_1);
-    wide = __any_sync(0xffffffffu, low < (uint32_t)max(top - SPREAD, 0) << 23);
+  }
+  // The sample is wide if any lane's scales are apart.  Once they are, they stay so.
+  template <int SPREAD> MARCHE_DEVINL bool apart() const { return low < (uint32_t)max(top - SPREAD, 0) << 23; }
+  // The unit for what has been seen, by all lanes of the warp; returns by how many powers of two it rises.
+  MARCHE_DEVINL int move(bool is_wide, bool first) {
+    wide = is_wide;
     const int before = first ? top : unit;
     int d = top - before;
     if (__builtin_expect(wide, 0)) {

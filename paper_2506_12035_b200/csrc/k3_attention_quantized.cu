@@ -292,61 +292,71 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
       }
       // ---- references: the unit above the value scales, the rows' maxima
       const uint32_t v0 = __float_as_uint(vs[lane]), v1 = KT == 64 ? __float_as_uint(vs[lane + KT / 2]) : v0;
-      const int d = units.take<kSpread>(__reduce_max_sync(0xffffffffu, max(v0, v1)), min(v0 - 1u, v1 - 1u), u == 0);
-      const float lift = pow2(267 - units.unit);           // 2^14 over the power of two above the scale
-      const float falls = units.wide ? (float)d : 0.f;
-      float most[NB][2], neg[NB][2], corr[NB][2];
-      bool moved = d != 0;
-#pragma unroll
-      for (int m = 0; m < NB; ++m)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) most[m][r] = m_run[m][r] - falls;
-      if (__builtin_expect(!units.wide, 1)) {
-#pragma unroll
-        for (int i = 0; i < NM; ++i)
-#pragma unroll
-          for (int m = 0; m < NB; ++m)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) most[m][r] = max3(most[m][r], sacc[m][i][r], sacc[m][i][2 + r]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < NM; ++i) {
-          const float a0 = attq::counts(vs[16 * i + g] * lift * 0x1p-14f), a1 = attq::counts(vs[16 * i + g + 8] * lift * 0x1p-14f);
-#pragma unroll
-          for (int m = 0; m < NB; ++m)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) most[m][r] = max3(most[m][r], sacc[m][i][r] + a0, sacc[m][i][2 + r] + a1);
-        }
-      }
+      units.see(__reduce_max_sync(0xffffffffu, max(v0, v1)), min(v0 - 1u, v1 - 1u));
+      const bool apart = units.apart<kSpread>();
+      bool moved = apart || units.top != units.unit;
+      float most[NB][2], neg[NB][2];
+      auto over_lanes = [&](float& mx) {
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+      };
 #pragma unroll
       for (int m = 0; m < NB; ++m)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const float before = m_run[m][r] - falls;
-          float mx = most[m][r];
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          const float ref = mx == -INFINITY ? 0.f : mx;
-          corr[m][r] = ex2_approx(before - ref);
-          moved = moved || mx != before;
-          m_run[m][r] = mx;
-          neg[m][r] = -ref;
+          most[m][r] = m_run[m][r];
+#pragma unroll
+          for (int i = 0; i < NM; ++i) most[m][r] = max3(most[m][r], sacc[m][i][r], sacc[m][i][2 + r]);
+          over_lanes(most[m][r]);
+          moved = moved || most[m][r] != m_run[m][r];
         }
       if (__any_sync(0xffffffffu, moved)) {
-        const float step = units.wide ? 1.f : attq::step_of(d), step_l = units.wide ? pow2(127 + d) : 1.f;
+        const int d = units.move(__any_sync(0xffffffffu, apart), u == 0);
+        float step_l = 1.f;
+        if (__builtin_expect(units.wide, 0)) {             // other references than the rows' largest logits
+          const float over_unit = pow2(max(253 - units.unit, 1));
+          step_l = pow2(127 + d);
+#pragma unroll
+          for (int m = 0; m < NB; ++m) most[m][0] = m_run[m][0] -= (float)d, most[m][1] = m_run[m][1] -= (float)d;
+#pragma unroll
+          for (int i = 0; i < NM; ++i) {
+            const float a0 = attq::counts(vs[16 * i + g] * over_unit), a1 = attq::counts(vs[16 * i + g + 8] * over_unit);
+#pragma unroll
+            for (int m = 0; m < NB; ++m)
+#pragma unroll
+              for (int r = 0; r < 2; ++r) most[m][r] = max3(most[m][r], sacc[m][i][r] + a0, sacc[m][i][2 + r] + a1);
+          }
+#pragma unroll
+          for (int m = 0; m < NB; ++m) {
+            over_lanes(most[m][0]);
+            over_lanes(most[m][1]);
+          }
+        }
+        const float step = units.wide ? 1.f : attq::step_of(d);
 #pragma unroll
         for (int m = 0; m < NB; ++m) {
-          mul2(l_run[m][0], l_run[m][1], corr[m][0], corr[m][1]);
+          float corr[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            corr[r] = ex2_approx(m_run[m][r] - (most[m][r] == -INFINITY ? 0.f : most[m][r]));
+            m_run[m][r] = most[m][r];
+          }
+          mul2(l_run[m][0], l_run[m][1], corr[0], corr[1]);
           mul2(l_run[m][0], l_run[m][1], step_l, step_l);
-          mul2(corr[m][0], corr[m][1], step, step);
+          mul2(corr[0], corr[1], step, step);
 #pragma unroll
           for (int c = 0; c < C::CHUNKS; ++c) {
-            mul2(oacc[m][c][0], oacc[m][c][1], corr[m][0], corr[m][1]);
-            mul2(oacc[m][c][2], oacc[m][c][3], corr[m][0], corr[m][1]);
+            mul2(oacc[m][c][0], oacc[m][c][1], corr[0], corr[1]);
+            mul2(oacc[m][c][2], oacc[m][c][3], corr[0], corr[1]);
           }
         }
       }
+      const float lift = pow2(267 - units.unit);           // 2^14 over the power of two above the scale
+#pragma unroll
+      for (int m = 0; m < NB; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) neg[m][r] = m_run[m][r] == -INFINITY ? 0.f : -m_run[m][r];
       // ---- weights, turned, and O^T += V^T P^T
       float ls[NB][2];
 #pragma unroll

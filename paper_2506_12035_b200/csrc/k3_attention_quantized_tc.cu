@@ -452,7 +452,8 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         const float ks = key < left ? raw_s[key] : 0.f, vs = key < left ? raw_s[KT + key] : 0.f;
         const uint32_t other = (key ^ 32) < left ? __float_as_uint(raw_s[KT + (key ^ 32)]) : 0u;
         const uint32_t mine = __float_as_uint(vs);
-        const int d = units.take<kSpread>(__reduce_max_sync(0xffffffffu, max(mine, other)), min(mine - 1u, other - 1u), kt == 0);
+        units.see(__reduce_max_sync(0xffffffffu, max(mine, other)), min(mine - 1u, other - 1u));
+        const int d = units.move(__any_sync(0xffffffffu, units.apart<kSpread>()), kt == 0);
         if (!wait(B_K_EMPTY + slot, phase)) { ok = false; break; }
         scale_slot[key] = ks * c_log2;
         scale_slot[KT + key] = vs * pow2(260 - units.unit);   // below 2^7, so that weights of up to 2^8 stay below fp16's end
