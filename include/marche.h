@@ -446,7 +446,7 @@ int marche_attention_two_segment(marche_ctx* ctx, const void* qkv, int ld, int n
  *   codes   int8  [2][batch][seq_len][n_kv_heads * head_dim]   ([0] holds K, [1] V; -127 .. 127)
  *   scales  float [2][batch][n_kv_heads][pad], pad = seq_len rounded up to a multiple of 64; the entries
  *           behind seq_len are neither read for their values nor written
- * head_dim 64, 80 or 128, seq_len up to MARCHE_QUANTIZED_MAX_SEQ and batch * n_kv_heads * head_dim below 2^30
+ * Codes of -128 and scales below 0 are read like the others.  head_dim 64, 80 or 128, seq_len up to MARCHE_QUANTIZED_MAX_SEQ and batch * n_kv_heads * head_dim below 2^30
  * (MARCHE_ESHAPE otherwise); both arrays 16-byte aligned device memory of the caller, of the sizes that the two
  * functions return (0 for dimensions that are not supported). */
 #define MARCHE_QUANTIZED_MAX_SEQ (1 << 24)

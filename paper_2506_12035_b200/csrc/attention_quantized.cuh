@@ -23,6 +23,7 @@ constexpr int kAboveLow = 50, kBelowTop = 75;
 constexpr float kBelow = 45.f;
 
 MARCHE_DEVINL float pow2(int biased_exponent) { return __int_as_float(biased_exponent << 23); }
+MARCHE_DEVINL uint32_t magnitude(float scale) { return __float_as_uint(scale) & 0x7fffffffu; }
 MARCHE_DEVINL float lg2_approx(float x) {
   float y;
   asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -46,13 +47,13 @@ MARCHE_DEVINL uint32_t finite_of(uint32_t w) {
   return max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u);
 }
 
-// The largest value scale so far and the unit, as biased exponents, and a lane's smallest scale so far that is not 0.
+// The largest value scale so far by magnitude and the unit, as biased exponents, and a lane's smallest scale so far that is not 0.
 struct Units {
   int top = 14, unit = 14;                                 // (14: the lowest whose factors exist)
   uint32_t low = 0xffffffffu;                              // as bits less 1
   bool wide = false;
-  // Takes in a tile's largest scale and the smallest that is not 0 of the lane's, less 1 (0xffffffff: none), as bits: scales are not negative, so
-  // they order as integers; NaN counts as the largest number.
+  // Takes in a tile's largest scale and the smallest that is not 0 of the lane's, less 1 (0xffffffff: none), as magnitudes' bits, which order as
+  // integers; NaN counts as the largest number.
   MARCHE_DEVINL void see(uint32_t largest, uint32_t smallest_less_1) {
     top = max(top, min((int)(largest >> 23), 254));
     low = min(low, smallest_less_1);
@@ -75,7 +76,7 @@ struct Units {
 // What O is multiplied by when the unit rises by d and the references stay (where it rises this far, O is nothing beside it).
 MARCHE_DEVINL float step_of(int d) { return d > 126 ? 0.f : pow2(127 - d); }
 // What a key's logit counts for its row's reference in a wide sample: log2 of its scale over the unit, at least -kBelow.
-MARCHE_DEVINL float counts(float scale_over_unit) { return fmaxf(lg2_approx(scale_over_unit), -kBelow); }
+MARCHE_DEVINL float counts(float scale_over_unit) { return fmaxf(lg2_approx(fabsf(scale_over_unit)), -kBelow); }
 
 // unit / l as two factors that leave fp32's range neither by themselves nor multiplied one after the other: 1 / l's mantissa, and the powers of two
 // (what of them is too small for one number goes to the first).  l 0 (no key): zeros; NaN stays.

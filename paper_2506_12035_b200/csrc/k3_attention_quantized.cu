@@ -292,7 +292,7 @@ attention_quantized_kernel(const __grid_constant__ CUtensorMap tmap, const __gri
           }
       }
       // ---- references: the unit above the value scales, the rows' maxima
-      const uint32_t v0 = __float_as_uint(vs[lane]), v1 = KT == 64 ? __float_as_uint(vs[lane + KT / 2]) : v0;
+      const uint32_t v0 = attq::magnitude(vs[lane]), v1 = KT == 64 ? attq::magnitude(vs[lane + KT / 2]) : v0;
       units.see(__reduce_max_sync(0xffffffffu, max(v0, v1)), min(v0 - 1u, v1 - 1u));
       const bool apart = units.apart<kSpread>();
       bool moved = apart || units.top != units.unit;

@@ -450,8 +450,8 @@ attention_quantized_tc_kernel(const __grid_constant__ CUtensorMap tmap, const bf
         const float* raw_s = reinterpret_cast<const float*>(gen + C::OFF_RAW) + (j * NSTG + stg) * 2 * KT;
         const int left = un.len - kt * KT;               // keys of this tile that count (behind them scales may be anything)
         const float ks = key < left ? raw_s[key] : 0.f, vs = key < left ? raw_s[KT + key] : 0.f;
-        const uint32_t other = (key ^ 32) < left ? __float_as_uint(raw_s[KT + (key ^ 32)]) : 0u;
-        const uint32_t mine = __float_as_uint(vs);
+        const uint32_t other = (key ^ 32) < left ? attq::magnitude(raw_s[KT + (key ^ 32)]) : 0u;
+        const uint32_t mine = attq::magnitude(vs);
         units.see(__reduce_max_sync(0xffffffffu, max(mine, other)), min(mine - 1u, other - 1u));
         const int d = units.move(__any_sync(0xffffffffu, units.apart<kSpread>()), kt == 0);
         if (!wait(B_K_EMPTY + slot, phase)) { ok = false; break; }

@@ -874,6 +874,20 @@ def test_weights_laid_out_on_another_stream(models):
 
 
 @pytest.mark.parametrize("dh,n", [(64, 1), (80, 30), (128, 3), (64, 140), (128, 150)])
+@pytest.mark.parametrize("power", [0, 40])
+def test_scales_of_either_sign_and_every_code(models, both_kernels, dh, n, power):
+    """A cache that others have filled: scales below 0, codes of -128; some value scales far below the rest."""
+    m, gen, B, S, H = models["f16"], gen_of(n + dh), 2, 300, 2
+    cache = filled_cache(m, gen, B, S, H, dh)
+    cache.codes.copy_(torch.randint(-128, 128, cache.codes.shape, generator=gen, device="cuda").to(torch.int8))
+    assert int(cache.codes.min()) == -128
+    cache.scales *= torch.where(torch.rand(cache.scales.shape, generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    cache.scales[1, 0, :, 7] *= 2.0 ** -power
+    q = (0.3 * randn(gen, B * n, H * dh)).to(torch.bfloat16)
+    assert_attention(attend(m, cache, q, H * dh, n, H, None), cache, q, n, H, None)
+
+
+@pytest.mark.parametrize("dh,n", [(64, 1), (80, 30), (128, 3), (64, 140), (128, 150)])
 def test_values_at_the_upper_end_of_the_range(models, both_kernels, dh, n):
     """V near the largest bf16 number: the mean is one, though the sum over the keys would not be."""
     m, gen, B, S, H = models["bf16"], gen_of(n + dh), 2, 1500, 2
