@@ -436,8 +436,10 @@ int marche_attention_two_segment(marche_ctx* ctx, const void* qkv, int ld, int n
                                  marche_stream stream);
 
 /* ---------------------------------------------------------------- a cache of 8 bits, weights of 4
- * For decoding of few rows, which is bound by the bytes of the cache and of the weight matrices.  The calls
- * stand beside marche_scatter_kv, marche_attention and marche_linear and take their sizes from their own
+ * Half and a quarter of the memory of the 16-bit forms.  Time is gained where those are bound by their bytes:
+ * projections of up to 32 rows by large matrices take a third; attention of one token per sample over a large cache
+ * somewhat less; attention of many rows takes longer than over a 16-bit cache, and so do projections of 64 rows and
+ * more by small matrices.  The calls stand beside marche_scatter_kv, marche_attention and marche_linear and take their sizes from their own
  * arguments, not from the context's shape; the context gives the element types (16-bit contexts only:
  * MARCHE_ESHAPE in a fp32 one), the device and the status word.  They need no workspace.
  * A call of no rows (n or M 0) checks its other arguments, enqueues nothing, and takes NULL for the rows. */
@@ -446,9 +448,10 @@ int marche_attention_two_segment(marche_ctx* ctx, const void* qkv, int ld, int n
  *   codes   int8  [2][batch][seq_len][n_kv_heads * head_dim]   ([0] holds K, [1] V; -127 .. 127)
  *   scales  float [2][batch][n_kv_heads][pad], pad = seq_len rounded up to a multiple of 64; the entries
  *           behind seq_len are neither read for their values nor written
- * Codes of -128 and scales below 0 are read like the others.  head_dim 64, 80 or 128, seq_len up to MARCHE_QUANTIZED_MAX_SEQ and batch * n_kv_heads * head_dim below 2^30
- * (MARCHE_ESHAPE otherwise); both arrays 16-byte aligned device memory of the caller, of the sizes that the two
- * functions return (0 for dimensions that are not supported). */
+ * Codes of -128 and scales below 0 are read like the others.  head_dim 64, 80 or 128, seq_len up to
+ * MARCHE_QUANTIZED_MAX_SEQ and batch * n_kv_heads * head_dim below 2^30 (MARCHE_ESHAPE otherwise); both arrays
+ * 16-byte aligned device memory of the caller, of the sizes that the two functions return (0 for dimensions that
+ * are not supported). */
 #define MARCHE_QUANTIZED_MAX_SEQ (1 << 24)
 typedef struct {
   int8_t* codes;
@@ -482,8 +485,10 @@ int marche_gather_kv_quantized(marche_ctx* ctx, const marche_quantized_cache* ca
  *           sample without keys gives zeros.
  *   o       A [batch*n][n_heads*head_dim] dense, 16-byte aligned
  * n_heads % n_kv_heads == 0 (MARCHE_EINVAL).  marche_tuning.attention_kernel forces the mma.sync or (both other
- * values) the tcgen05 kernel, AUTO picks by rows, keys, head_dim and items.  Relevance scores are not taken here: a block that yields them keeps a
- * 16-bit cache.  Every shape is bit-reproducible. */
+ * values) the tcgen05 kernel, AUTO picks by rows, keys, head_dim and items.  fp32 sums of exact products; a softmax weight is
+ * rounded to 11 bits relative to the row's largest product of weight and value scale, but for fp16 outputs of the mma.sync
+ * kernel, where the rest follows.  No row's values reach another row's result (rows of padding may hold anything).  Relevance
+ * scores are not taken here: a block that yields them keeps a 16-bit cache.  Every shape is bit-reproducible. */
 int marche_attention_quantized(marche_ctx* ctx, const void* q, int ld_q, int n, int n_heads,
                                const marche_quantized_cache* cache, const int32_t* kv_len, void* o, marche_stream stream);
 

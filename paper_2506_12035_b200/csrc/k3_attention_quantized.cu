@@ -8,7 +8,7 @@
 // accumulators are fp32, and the running exponent e moves with the running maximum (one factor for both).
 // Where the output is fp16, what that rounding left off follows as a second operand (FINE): with one rounding of as many bits as the output's own the
 // error is 1.4 times the output's, 1.55 over few keys.  A bf16 output, eight times coarser, does not need it (128 x 43 rows over 320 keys of 16
-// heads of 80: 64 us without, 72 with it).
+// heads of 80: 66 us without, 77 with it).
 // Query heads that share a cached head are rows of one item: row r is token r / G, head r % G of the group.
 //
 // mma.sync m16n8k16 on the transposed products, S^T = K q^T and O^T = V^T P^T: keys (then columns of V) are the 16-row operand and the
@@ -17,15 +17,16 @@
 // operands of four k16 steps (bytes 0 and 2 of a word, then 1 and 3): no transposition and one shared-memory load.  V: ldmatrix.trans on
 // pairs of bytes, whose even and odd bytes are rows g and g + 8 of the operand.  Codes become numbers (1024 + code + 128, minus 1152); as they
 // stand, code + 128 is a fp16 subnormal, which the tensor cores multiply exactly, but 128 times the sum of the other operand would
-// have to come off, and where that is of one sign the result loses as many bits as it is smaller (for K too: logits off by 2^-16 of the sum of
-// magnitudes where fp32 sums are by 2^-23; 128 x 43 rows 2 % slower, one token over 65521 keys 3 %).  P: the accumulator's layout is turned by movmatrix.
+// have to come off, and where that is of one sign the result loses as many bits as it is smaller (logits are then off by 2^-16 of the sum of
+// magnitudes, where fp32 sums are by 2^-23; it would save 2 % at 128 x 43 rows, 3 % at one token over 65521 keys).  P: the accumulator's layout is turned by movmatrix.
 // nr warps take 8 NB rows each; nk groups of them take the tiles of 32 or 64 keys (K, V and both scales, by TMA) in turn, each group with a
 // ring of nst stages that its first warp fills (slot and phase are stepped: a division in that place cost more than the tile); a cluster of cs
 // CTAs splits a long sequence.  (CTA, group) pairs merge in rank order in the CTA that owns the row: bit-reproducible.  A sample without
 // keys gives zeros.
 // What bounds it: with a row or a few, one warp's chain through a tile (2500 cycles for 32 keys of 128 values: wait, products, maxima over lanes,
-// exponentials, products, refill), of which the longest sample has most: 4 x 65521 keys at most, 8 cached heads of 128, one token: 88 us of 42 for the bytes.  With
-// more rows its instructions: the 128 x 43 rows above 64 us of 21, 52 % of the issue slots (16 warps on an SM instead of 12, at 128 registers, spill: 67).
+// exponentials, products, refill), and the cut by sample: at most eight CTAs work on a (sample, head), so the longest sample's finish alone: 4 x 65521
+// keys at most, 8 cached heads of 128, one token: 90 us of 42 for the bytes.  With more rows its instructions, a third of them conversions that the
+// warps of a tile repeat: the 128 x 43 rows above 66 us of 21, 54 % of the issue slots (16 warps on an SM instead of 12, at 128 registers, spill: slower).
 #include <cuda.h>
 
 #include "attention_common.cuh"
@@ -550,10 +551,10 @@ cudaError_t launch(const void* q, int ld_q, int n, int heads, const QuantizedKv&
 
 // Which kernel: by estimated time (us).  This one: a warp of 16 rows takes a tile of 64 keys in 0.3 us of an SM's time where the SMs are full (0.4 where
 // a warp or two are on each), and splits long sequences; the tcgen05 one 0.8 us for 128 rows, but not less than 1.3 us a tile in turn.  Measured, this
-// one and tcgen05, us: head_dim 64, 2048 items, S 320: 43 rows 61 and 67, 64 rows 75 and 68, 128 rows 152 and 83; 512 items, S 1088: 32 rows 46
-// and 47, 43 rows 53 and 49, 200 rows 189 and 104; 128 items 43 rows 22.2 and 24.6, 64 rows 27.7 and 24.2; 32 items 128 rows 21.5 and 23.6;
-// 24 items, S 5000, 200 rows 57 and 87; head_dim 80, 2048 items, S 320, 43 rows 68 and 75; head_dim 128, 512 items, S 1088, 32 rows 74 and 98, 64
-// rows 126 and 101.
+// one and tcgen05, us: head_dim 64, 2048 items, S 320: 43 rows 61 and 63, 64 rows 76 and 66, 128 rows 156 and 81; 512 items, S 1088: 32 rows 42.4
+// and 42.9, 43 rows 52 and 44, 200 rows 191 and 97; 128 items 43 rows 22.4 and 22.2, 64 rows 27.6 and 22.4; 32 items 128 rows 21.5 and 21.6;
+// 24 items, S 5000, 200 rows 58 and 81; head_dim 80, 2048 items, S 320, 43 rows 66 and 70; head_dim 128, 512 items, S 1088, 32 rows 74 and 91, 64
+// rows 122 and 94.  The choice costs 3 % at most at 20 measured shapes.
 bool attention_quantized_tc_wins(int R, int S, int dh, int items) {
   if (R <= 16) return false;
   const double sms = device_sm_count(), tiles = (S + 63) / 64, warp_tiles = (double)items * ((R + 15) / 16) * tiles / sms, units = (double)items * ((R + 127) / 128);

@@ -1,7 +1,9 @@
 // K3 over a cache held in 8 bits, many query rows: the products on the 5th-generation tensor cores, one conversion of the codes for 128 rows.
 //
-// The mathematics and the roundings are those of the mma.sync kernel (k3_attention_quantized.cu): codes are multiplied as exact fp16
-// numbers, a key's scale multiplies its logits, its value scale its weight before the weight's only rounding.  What that kernel is bound by from some
+// The mathematics is that of the mma.sync kernel (k3_attention_quantized.cu): codes are multiplied as exact fp16 numbers, a key's scale
+// multiplies its logits, its value scale its weight before that is rounded to fp16.  Here weights are lifted by 2^7 only, since the reference lags by up
+// to 2^8, and there is no second operand for what the rounding left off (it would take the columns and the instructions of a second P V): the error of
+// fp16 outputs is 1.4 times the output's own rounding, where the mma.sync kernel's is that rounding alone.  What that kernel is bound by from some
 // 32 rows on is its own instructions (1000 to 1500 of a warp for 64 keys x 32 rows, a third of them conversions that every warp repeats).  Here
 // a warp pair converts a tile once for a unit of 128 rows, and a thread owns a row of the softmax.
 // Persistent CTAs, one per SM; unit = 128 rows (tokens x query heads of a group) of one (sample, cached head) against all of its
@@ -11,11 +13,13 @@
 //      written back to tensor memory as the A operand of P V
 //   2  converters: the unit's query rows (fp16, divided by a power of two), then per tile K and V from bytes to swizzled
 //      fp16 operand tiles (two of each), the scales, and the running exponent above all value scales, which the weights are relative
-//      to.  (Four of them, or a third stream, take registers from the softmax: 484 and 492 us where two streams of two took 424.)
+//      to.  (Four of them, or a third stream, take registers from the softmax: 484 and 492 us where two streams of two took 424.)  Every 128 rows
+//      of an item convert its tiles again.
 //   1  TMA producer: codes and scales of the tiles into a staging ring
 //   1  issues tcgen05.mma: S = Q K^T (M128 x N64), O += P V (V as an MN-major operand); S of the next tile runs under the softmax of this one
-// What bounds it: the softmax warps' instructions; of them the exponentials, 16 per clock and SM, take 512 cycles for a tile of 64 x 128.  32 samples x 1088 rows
-// over 1088 keys, 16 heads of 64: 400 us, of which the exponentials alone 140 and the products 94.
+// What bounds it: the chain of a stream's tile, softmax (of it the exponentials, 16 per clock and SM, 512 cycles for a tile of 64 x 128), conversion and products
+// in turn, with two streams to fill the gaps (46 % of the issue slots).  32 samples x 1088 rows over 1088 keys, 16 heads of 64: 405 us, of which the
+// exponentials alone 140 and the products 94.  Where rows need powers of two of their own 454, where value scales lie far apart 630.
 // All waits are bounded and report through the status word.
 #include <cuda.h>
 
